@@ -254,8 +254,9 @@ srigl_status srigl_fwd_plan_query_algo(int32_t B, int32_t d_in, int32_t n_active
  * Sec. 3.1 (neuron ablation reduces the width of a layer) and App. H (the timed layer is one linear of a ViT MLP
  * block: linear, GELU, linear).  srigl_condensed_linear_fwd_act is the forward call with an activation applied to
  * every written value, stored and ablated columns alike (an ablated neuron outputs act(bias)); SRIGL_ACT_GELU is
- * v * Phi(v) with the normal distribution function (erf form). */
-typedef enum srigl_activation { SRIGL_ACT_NONE = 0, SRIGL_ACT_RELU = 1, SRIGL_ACT_GELU = 2 } srigl_activation;
+ * v * Phi(v) with the normal distribution function (erf form).  SRIGL_ACT_SILU, v times its logistic function, is for the structured-only layer with an
+ * epilogue and the gated block (srigl_structured_linear_fwd_act, srigl_gated_linear_fwd and their gradients); the other calls refuse it. */
+typedef enum srigl_activation { SRIGL_ACT_NONE = 0, SRIGL_ACT_RELU = 1, SRIGL_ACT_GELU = 2, SRIGL_ACT_SILU = 3 } srigl_activation;
 
 /* The forward call in the whole-input batched kernel (SRIGL_FWD_ROWLOOP) in a tile of 8, 16, 32 or 64 batch rows (0: the library's
  * choice) with rows_per_wave stored rows to a wavefront (0: likewise) and xcd_order as in srigl_fwd_tuning, on rows of any length
@@ -468,6 +469,53 @@ srigl_status srigl_structured_linear_fwd_split(const void* x, srigl_dtype x_dtyp
                                                srigl_dtype w_dtype, const int32_t* active, int32_t n_active, const float* bias,
                                                int32_t d_out, float* y, srigl_gemm_tile tile, int32_t splits, void* workspace,
                                                size_t workspace_bytes, void* stream);
+
+/* ---- feed-forward blocks in the structured-only form, forward and backward ----------------------------------
+ * Sec. 3.1 / App. H: the linear layers of a block with what stands between them, for inference and for training: the connectivity update
+ * ranks the dense gradient of the loss with respect to W, which is what srigl_structured_linear_bwd returns (in fp32 storage as the update takes it).
+ * Common to the four calls: x_dtype == w_dtype, called the storage type; sums in fp32; matrices dense and row-major, of any size (at most 2^30 a side, 2^29
+ * neurons in a backward pass) and from any element's address on (16-byte aligned operands whose rows are multiples of 16 bytes run faster); outputs fully
+ * overwritten, in rounding to nearest, and not aliasing inputs unless said otherwise; workspace: device memory of the caller, 16-byte aligned, at least as many bytes as the
+ * call's query says (host arithmetic on the same sizes; NULL where that is 0), contents undefined afterwards, SRIGL_ERR_CAPACITY where it is
+ * smaller.  Calls that share one must not overlap.  No call synchronises, allocates or uses atomics: the same inputs give the same bits.
+ *
+ * srigl_structured_linear_fwd_act:
+ *   z[b][s] = bias[active[s]] + sum_j Wd[s][j] x[b][j];  y[b][active[s]] = act(z[b][s]) + residual[b][active[s]];  other columns: act(bias[c]) + residual[b][c].
+ *   active, bias as in srigl_structured_linear_fwd; residual[B][d_out] of y_dtype or NULL, may be y itself; y[B][d_out] of y_dtype, the storage type or fp32; z
+ *   (may be NULL): [B][n_active] of the storage type, what the backward pass takes.
+ * srigl_structured_linear_bwd: with dz[b][s] = dy[b][active[s]] act'(z[b][s]),
+ *   dx[B][d_in] = dz Wd and dWd[n_active][d_in] = dz^T x of the storage type, dbias[d_out] fp32: sum_b dz[b][s] at active[s], act'(bias[c]) sum_b dy[b][c] at the
+ *   others.  dy[B][d_out] of dy_dtype, the storage type or fp32 (the gradient of the residual is dy itself).  Outputs may be NULL (not wanted), with them Wd, x; z may be
+ *   with SRIGL_ACT_NONE; bias is read for ablated neurons only.  In bf16 dz is rounded to bf16 before the products (the matrix units' type); dbias sums it unrounded.
+ *   The slope of SRIGL_ACT_RELU is 0 at 0. */
+size_t srigl_structured_act_workspace_bytes(int32_t B, int32_t d_in, int32_t n_active, srigl_dtype dtype);
+
+srigl_status srigl_structured_linear_fwd_act(const void* x, srigl_dtype x_dtype, int32_t B, int32_t d_in, const void* Wd, srigl_dtype w_dtype,
+                                             const int32_t* active, int32_t n_active, const float* bias, const void* residual, int32_t d_out, void* y,
+                                             srigl_dtype y_dtype, void* z, srigl_activation act, void* workspace, size_t workspace_bytes, void* stream);
+
+size_t srigl_structured_bwd_workspace_bytes(int32_t B, int32_t d_in, int32_t n_active, int32_t d_out, srigl_dtype dtype);
+
+srigl_status srigl_structured_linear_bwd(const void* dy, srigl_dtype dy_dtype, const void* x, srigl_dtype x_dtype, int32_t B, int32_t d_in, const void* Wd,
+                                         srigl_dtype w_dtype, const int32_t* active, int32_t n_active, const float* bias, const void* z, int32_t d_out,
+                                         srigl_activation act, void* dx, void* dWd, float* dbias, void* workspace, size_t workspace_bytes, void* stream);
+
+/* The gated block: h[b][c] = act(g[b][c]) u[b][c] with g = x Wg^T + bias_g and u = x Wu^T + bias_u, both products in one launch.  Wg, Wu [n][d_in]: the stored
+ * neurons' rows (a hidden neuron is ablated in both); bias_g, bias_u [n] fp32 or NULL; h[B][n], and g and u (both or neither may be NULL; for the backward
+ * pass) of the storage type.  h is computed from the sums before they are rounded into g and u.
+ * srigl_gated_linear_bwd: with dg = dh u act'(g) and du = dh act(g), dx[B][d_in] = dg Wg + du Wu, dWg = dg^T x, dWu = du^T x [n][d_in] of the storage type, dbias_g,
+ * dbias_u [n] fp32 the column sums of dg and du; g and u as the forward pass left them, dh[B][n] of the storage type.  Outputs may be NULL; roundings as above. */
+size_t srigl_gated_workspace_bytes(int32_t B, int32_t d_in, int32_t n, srigl_dtype dtype);
+
+srigl_status srigl_gated_linear_fwd(const void* x, srigl_dtype x_dtype, int32_t B, int32_t d_in, const void* Wg, const void* Wu, srigl_dtype w_dtype, int32_t n,
+                                    const float* bias_g, const float* bias_u, srigl_activation act, void* h, void* g, void* u, void* workspace,
+                                    size_t workspace_bytes, void* stream);
+
+size_t srigl_gated_bwd_workspace_bytes(int32_t B, int32_t d_in, int32_t n, srigl_dtype dtype);
+
+srigl_status srigl_gated_linear_bwd(const void* dh, const void* x, srigl_dtype x_dtype, int32_t B, int32_t d_in, const void* Wg, const void* Wu,
+                                    srigl_dtype w_dtype, int32_t n, const void* g, const void* u, srigl_activation act, void* dx, void* dWg, void* dWu,
+                                    float* dbias_g, float* dbias_u, void* workspace, size_t workspace_bytes, void* stream);
 
 /* Which of the two representations of a layer is expected to run its forward pass faster for a batch of B rows
  * (Sec. 4.4 / Fig. 4: the condensed form wins at small batch and high sparsity, the structured-only form at large batch

@@ -19,7 +19,7 @@ LIB_PATH = os.path.join(_PKG, "libsrigl.so")
 OK, ERR_INVALID_ARG, ERR_FANIN, ERR_CAPACITY, ERR_INDEX_RANGE, ERR_UNSUPPORTED, ERR_HIP = range(7)
 F32, BF16 = 0, 1
 REPR_CONDENSED, REPR_STRUCTURED = 0, 1
-ACT_NONE, ACT_RELU, ACT_GELU = 0, 1, 2
+ACT_NONE, ACT_RELU, ACT_GELU, ACT_SILU = 0, 1, 2, 3   # ACT_SILU: the structured-only layer with an epilogue and the gated block only
 FWD_AUTO, FWD_GENERIC, FWD_KLANE, FWD_ROWLANE, FWD_ROWLOOP = range(5)
 TILE_AUTO, TILE_256x256, TILE_256x256_H, TILE_256x128_W4, TILE_256x128, TILE_128x128, TILE_64x64 = range(7)
 TILE_256x192, TILE_192x192, TILE_128x96, TILE_64x128 = range(7, 11)   # bf16, the library's own choice only
@@ -38,6 +38,8 @@ EXPORTS = (
     "srigl_compact_hidden_layer", "srigl_condensed_mlp_fwd", "srigl_narrow_idx", "srigl_condensed_linear_fwd_idx16", "srigl_csr_linear_fwd", "srigl_fwd_plan_query", "srigl_fwd_plan_query_algo",
     "srigl_condensed_linear_fwd_tile", "srigl_fwd_tile_query", "srigl_structured_tile_query",
     "srigl_blocked_bytes", "srigl_block_terms", "srigl_blocked_tile", "srigl_blocked_tile_with_copy", "srigl_blocked_linear_fwd",
+    "srigl_structured_act_workspace_bytes", "srigl_structured_linear_fwd_act", "srigl_structured_bwd_workspace_bytes", "srigl_structured_linear_bwd",
+    "srigl_gated_workspace_bytes", "srigl_gated_linear_fwd", "srigl_gated_bwd_workspace_bytes", "srigl_gated_linear_bwd",
 )
 
 
@@ -150,6 +152,17 @@ def _load() -> ctypes.CDLL:
     lib.srigl_blocked_tile_with_copy.argtypes = [i32, i32, i32, i32, i32]
     lib.srigl_blocked_linear_fwd.restype = ctypes.c_int
     lib.srigl_blocked_linear_fwd.argtypes = [vp, i32, i32, vp, vp, vp, i32, vp, i32, i32, vp, i32, vp, ctypes.c_int, i32, vp]
+    ci = ctypes.c_int
+    for name, res, args in (
+            ("srigl_structured_act_workspace_bytes", sz, [i32, i32, i32, ci]),
+            ("srigl_structured_linear_fwd_act", ci, [vp, ci, i32, i32, vp, ci, vp, i32, vp, vp, i32, vp, ci, vp, ci, vp, sz, vp]),
+            ("srigl_structured_bwd_workspace_bytes", sz, [i32, i32, i32, i32, ci]),
+            ("srigl_structured_linear_bwd", ci, [vp, ci, vp, ci, i32, i32, vp, ci, vp, i32, vp, vp, i32, ci, vp, vp, vp, vp, sz, vp]),
+            ("srigl_gated_workspace_bytes", sz, [i32, i32, i32, ci]),
+            ("srigl_gated_linear_fwd", ci, [vp, ci, i32, i32, vp, vp, ci, i32, vp, vp, ci, vp, vp, vp, vp, sz, vp]),
+            ("srigl_gated_bwd_workspace_bytes", sz, [i32, i32, i32, ci]),
+            ("srigl_gated_linear_bwd", ci, [vp, vp, ci, i32, i32, vp, vp, ci, i32, vp, vp, ci, vp, vp, vp, vp, vp, vp, sz, vp])):
+        getattr(lib, name).restype, getattr(lib, name).argtypes = res, args
     lib.srigl_launch_empty.restype = ctypes.c_int
     lib.srigl_launch_empty.argtypes = [vp]
     lib.srigl_copy_bytes.restype = ctypes.c_int
@@ -429,6 +442,53 @@ def srigl_mask_update_workspace_bytes(d_out: int, d_in: int) -> int:
 def srigl_mask_update(W, mask, grad, d_out, d_in, k, K_upd, gamma_percent, budget, mask_out, W_out, workspace, report):
     """report: int64[4] device tensor -> {k', remaining neurons, ablated by this update, pruned in step 6}."""
     _front.mask_update(W, mask, grad, d_out, d_in, k, K_upd, gamma_percent, budget, mask_out, W_out, workspace, report)
+
+
+def srigl_structured_act_workspace_bytes(B, d_in, n_active, dtype_code) -> int:
+    return int(lib.srigl_structured_act_workspace_bytes(int(B), int(d_in), int(n_active), int(dtype_code)))
+
+
+def srigl_structured_linear_fwd_act(x, B, d_in, Wd, active, n_active, bias, residual, d_out, y, z=None, act=ACT_NONE, workspace=None):
+    """y's type says whether the result is of the storage type or fp32; residual of y's type (or y itself), z of the storage type."""
+    assert residual is None or _dtype_code(residual) == _dtype_code(y)
+    assert z is None or _dtype_code(z) == _dtype_code(x)
+    _check(lib.srigl_structured_linear_fwd_act(_ptr(x), _dtype_code(x), int(B), int(d_in), _ptr(Wd), _dtype_code(Wd), _ptr(active), int(n_active), _ptr(bias),
+                                               _ptr(residual), int(d_out), _ptr(y), _dtype_code(y), _ptr(z), int(act), _ptr(workspace), _nbytes(workspace), _stream()),
+           "srigl_structured_linear_fwd_act")
+
+
+def srigl_structured_bwd_workspace_bytes(B, d_in, n_active, d_out, dtype_code) -> int:
+    return int(lib.srigl_structured_bwd_workspace_bytes(int(B), int(d_in), int(n_active), int(d_out), int(dtype_code)))
+
+
+def srigl_structured_linear_bwd(dy, x, B, d_in, Wd, active, n_active, bias, z, d_out, dx, dWd, dbias, workspace, act=ACT_NONE):
+    """dx, dWd, dbias: None where not wanted."""
+    assert all(t is None or _dtype_code(t) == _dtype_code(x) for t in (z, dx, dWd))
+    _check(lib.srigl_structured_linear_bwd(_ptr(dy), _dtype_code(dy), _ptr(x), _dtype_code(x), int(B), int(d_in), _ptr(Wd), _dtype_code(Wd), _ptr(active),
+                                           int(n_active), _ptr(bias), _ptr(z), int(d_out), int(act), _ptr(dx), _ptr(dWd), _ptr(dbias), _ptr(workspace),
+                                           _nbytes(workspace), _stream()), "srigl_structured_linear_bwd")
+
+
+def srigl_gated_workspace_bytes(B, d_in, n, dtype_code) -> int:
+    return int(lib.srigl_gated_workspace_bytes(int(B), int(d_in), int(n), int(dtype_code)))
+
+
+def srigl_gated_linear_fwd(x, B, d_in, Wg, Wu, n, bias_g, bias_u, h, g=None, u=None, act=ACT_SILU, workspace=None):
+    assert all(t is None or _dtype_code(t) == _dtype_code(x) for t in (Wu, h, g, u))
+    _check(lib.srigl_gated_linear_fwd(_ptr(x), _dtype_code(x), int(B), int(d_in), _ptr(Wg), _ptr(Wu), _dtype_code(Wg), int(n), _ptr(bias_g), _ptr(bias_u), int(act),
+                                      _ptr(h), _ptr(g), _ptr(u), _ptr(workspace), _nbytes(workspace), _stream()), "srigl_gated_linear_fwd")
+
+
+def srigl_gated_bwd_workspace_bytes(B, d_in, n, dtype_code) -> int:
+    return int(lib.srigl_gated_bwd_workspace_bytes(int(B), int(d_in), int(n), int(dtype_code)))
+
+
+def srigl_gated_linear_bwd(dh, x, B, d_in, Wg, Wu, n, g, u, dx, dWg, dWu, dbias_g, dbias_u, workspace, act=ACT_SILU):
+    """dx, dWg, dWu, dbias_g, dbias_u: None where not wanted."""
+    assert all(t is None or _dtype_code(t) == _dtype_code(x) for t in (dh, Wu, g, u, dx, dWg, dWu))
+    _check(lib.srigl_gated_linear_bwd(_ptr(dh), _ptr(x), _dtype_code(x), int(B), int(d_in), _ptr(Wg), _ptr(Wu), _dtype_code(Wg), int(n), _ptr(g), _ptr(u), int(act),
+                                      _ptr(dx), _ptr(dWg), _ptr(dWu), _ptr(dbias_g), _ptr(dbias_u), _ptr(workspace), _nbytes(workspace), _stream()),
+           "srigl_gated_linear_bwd")
 
 
 def srigl_launch_empty():

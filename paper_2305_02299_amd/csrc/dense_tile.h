@@ -1,0 +1,419 @@
+// Dense products on the matrix cores whose operands lie either way in memory (device side): what the forward and backward passes of the
+// structured-only layer and of the gated block share.
+//
+// A product is C[m][n] = sum_k A(m, k) B(n, k) over a BM x BN tile per workgroup, K walked in stages of 128 bytes of K a line.  An operand's
+// lines either run along K (a row of x against a row of W: forward) or across it (row k of W holds the k-th value of every column: the gradient of x
+// takes W this way, the gradient of W both operands).  The matrix units want eight consecutive k of one row in a lane's register pair.  Lines along K give
+// them with one 16-byte read of the LDS; for lines across K in bf16 the LDS hands four lines' values of a column to a lane (ds_read_b64_tr_b16: of 16 lanes,
+// lane i reads 8 bytes, columns 4 (i % 4) .. + 3 of line i / 4, and gets the values of column i in lines 0 .. 3), in fp32 a lane reads its four k as words.
+//
+// LDS layouts of a stage of R tile rows (R * 128 bytes): along K, row r at r * 128, its 16-byte piece q in slot q ^ ((r >> 1) & 7); across K, line k at
+// k * R * sizeof(T), its piece q in slot q ^ across_swizzle(k): the lines that one read touches lie in different banks.
+// MFMA operands: bf16 32x32x16, lane l holds row l % 32, k = 8 (l / 32) .. + 7 of a 32-byte step; fp32 32x32x2, lane l row l % 32, k = 4 (l / 32) + j in
+// the j-th of four.  Result: register e of lane l is row 8 (e / 4) + 4 (l / 32) + e % 4, column l % 32.
+#pragma once
+#include "mma_tile.h"
+#include <initializer_list>
+
+namespace srigl {
+
+typedef float f32x4_t __attribute__((ext_vector_type(4)));
+typedef short s16x4_t __attribute__((ext_vector_type(4)));
+
+template <typename T> struct DenseFrag;
+template <> struct DenseFrag<uint16_t> { using type = bf16x8_t; };
+template <> struct DenseFrag<float> { using type = f32x4_t; };
+__device__ __forceinline__ void dense_mma(f32x16_t& acc, const bf16x8_t& a, const bf16x8_t& b) { acc = __builtin_amdgcn_mfma_f32_32x32x16_bf16(a, b, acc, 0, 0, 0); }
+__device__ __forceinline__ void dense_mma(f32x16_t& acc, const f32x4_t& a, const f32x4_t& b) {
+#pragma unroll
+    for (int j = 0; j < 4; ++j) acc = __builtin_amdgcn_mfma_f32_32x32x2f32(a[j], b[j], acc, 0, 0, 0);
+}
+
+constexpr int kLineBytes = 128;                                              // of K a stage
+template <typename T> constexpr int kStageK = kLineBytes / (int)sizeof(T);   // its elements
+template <typename T> constexpr int kPiece = 16 / (int)sizeof(T);            // elements of a 16-byte piece
+
+// Loads and stores of V consecutive elements from any element's address
+template <typename T, int V> struct AnyPlace { typedef T type __attribute__((ext_vector_type(V), aligned(sizeof(T)))); };
+
+// ---- operands: line(l, first, valid) is where elements first .. of line l begin, *valid how many of them there are (<= 0: none) ----
+// Along K: line = tile row, elements = k.
+template <typename T> struct RowsOf {
+    static constexpr bool kAlong = true;
+    const T* base;      // of the tile's first row
+    long long pitch;
+    int last, K;        // last row that there is, counted from the tile's first
+    __device__ void move(int first) { base += (size_t)first * pitch; last -= first; }
+    __device__ const T* line(int l, int first, int* valid) const { *valid = K - first; return base + (size_t)min(l, last) * pitch + first; }
+};
+// The weight rows of two matrices that a gated block multiplies with, next to each other in each wavefront's part of the tile: HALF rows of the first,
+// the same HALF rows of the second.
+template <typename T, int HALF> struct PairedRows {
+    static constexpr bool kAlong = true;
+    const T *base, *second;
+    long long pitch;
+    int last, K;
+    __device__ void move(int first) { base += (size_t)first * pitch; second += (size_t)first * pitch; last -= first; }
+    __device__ const T* line(int l, int first, int* valid) const {
+        const int part = l / HALF, r = (part >> 1) * HALF + l % HALF;
+        *valid = K - first;
+        return ((part & 1) ? second : base) + (size_t)min(r, last) * pitch + first;
+    }
+};
+// Across K: line = k, elements = tile columns.
+template <typename T> struct ColsOf {
+    static constexpr bool kAlong = false;
+    const T* base;      // of the tile's first column, line 0
+    long long pitch;
+    int cols, K;        // columns from there on
+    __device__ void move(int first) { base += first; cols -= first; }
+    __device__ const T* line(int l, int first, int* valid) const { *valid = l < K ? cols - first : 0; return base + (size_t)l * pitch + first; }
+};
+// Lines 0 .. n - 1 of one matrix, then, from line `padded` on, those of a second.
+template <typename T> struct PairedCols {
+    static constexpr bool kAlong = false;
+    const T *base, *second;
+    long long pitch;
+    int cols, n, padded;
+    __device__ void move(int first) { base += first; second += first; cols -= first; }
+    __device__ const T* line(int l, int first, int* valid) const {
+        const bool behind = l >= padded;
+        const int r = behind ? l - padded : l;
+        *valid = r < n ? cols - first : 0;
+        return (behind ? second : base) + (size_t)r * pitch + first;
+    }
+};
+
+// 16 bytes from there, zeros behind the valid elements
+template <typename T>
+__device__ __forceinline__ uint4 load_piece(const T* p, int valid) {
+    if (valid >= kPiece<T>) {
+        typename AnyPlace<T, kPiece<T>>::type v = *reinterpret_cast<const typename AnyPlace<T, kPiece<T>>::type*>(p);
+        return __builtin_bit_cast(uint4, v);
+    }
+    uint32_t w[4] = {0u, 0u, 0u, 0u};
+#pragma unroll
+    for (int e = 0; e < kPiece<T>; ++e)
+        if (e < valid) {
+            if constexpr (sizeof(T) == 4) w[e] = __float_as_uint(p[e]);
+            else w[e >> 1] |= (uint32_t)p[e] << (16 * (e & 1));
+        }
+    return make_uint4(w[0], w[1], w[2], w[3]);
+}
+
+// Slot of piece q of line k, lines across K of R columns.  bf16: a read takes four lines (k % 4 = 0 .. 3) and 64 bytes of each: the 64-byte quarters of
+// 256 bytes are exchanged by the line; of 128-byte lines two share 256 bytes.  fp32: lines k and k + 4, 128 bytes of each.
+template <typename T, int R>
+__device__ __forceinline__ int across_swizzle(int k) {
+    if constexpr (sizeof(T) == 4) return ((k >> 2) & 1) << 3;
+    else return R >= 128 ? (k & 3) << 2 : ((k >> 1) & 1) << 2;
+}
+
+// Byte offset, in a stage of R rows at 0, of what lane l reads for step kk of the 32-row block at row 0; other blocks: + block_offset.
+template <typename T, bool ALONG, int R>
+struct FragReader {
+    using F = typename DenseFrag<T>::type;
+    static constexpr int PITCH = R * (int)sizeof(T);
+    __device__ static F read(const unsigned char* stage, int block, int kk, int lane) {
+        const int half = lane >> 5, r = lane & 31;
+        if constexpr (ALONG) {
+            const int row = block * 32 + r;
+            return *reinterpret_cast<const F*>(stage + row * kLineBytes + (((2 * kk + half) ^ ((row >> 1) & 7)) << 4));
+        } else if constexpr (sizeof(T) == 4) {
+            F f;
+            const int c = block * 32 + r;
+#pragma unroll
+            for (int j = 0; j < 4; ++j) {
+                const int k = 8 * kk + 4 * half + j;
+                f[j] = *reinterpret_cast<const float*>(stage + k * PITCH + ((((c >> 2) ^ across_swizzle<T, R>(k)) << 4) | ((c & 3) << 2)));
+            }
+            return f;
+        } else {
+            const int i = lane & 15, c = block * 32 + (lane & 16) + 4 * (i & 3);
+            union { s16x4_t part[2]; F f; } u;
+#pragma unroll
+            for (int s = 0; s < 2; ++s) {
+                const int k = 16 * kk + 8 * half + 4 * s + (i >> 2);
+                const unsigned char* at = stage + k * PITCH + ((((c >> 3) ^ across_swizzle<T, R>(k)) << 4) | ((c & 4) << 1));
+                u.part[s] = __builtin_amdgcn_ds_read_tr16_b64_v4i16((__attribute__((address_space(3))) s16x4_t*)at);
+            }
+            return u.f;
+        }
+    }
+};
+
+// ---- the product of a tile, staged through registers: any address, any size ----
+template <typename T, int R, int NT, class Op>
+struct RegStage {
+    static constexpr int PASSES = R * kLineBytes / 16 / NT, PER_LINE = Op::kAlong ? 8 : R / kPiece<T>;
+    static_assert(R * kLineBytes % (16 * NT) == 0, "pieces to a thread");
+    uint4 held[PASSES];
+    __device__ void load(const Op& op, int h) {
+#pragma unroll
+        for (int p = 0; p < PASSES; ++p) {
+            const int u = p * NT + threadIdx.x, l = u / PER_LINE, q = u % PER_LINE;
+            int valid;
+            const T* at = Op::kAlong ? op.line(l, h * kStageK<T> + q * kPiece<T>, &valid) : op.line(h * kStageK<T> + l, q * kPiece<T>, &valid);
+            held[p] = load_piece(at, valid);
+        }
+    }
+    __device__ void store(unsigned char* stage) const {
+#pragma unroll
+        for (int p = 0; p < PASSES; ++p) {
+            const int u = p * NT + threadIdx.x, l = u / PER_LINE, q = u % PER_LINE;
+            const int slot = Op::kAlong ? q ^ ((l >> 1) & 7) : q ^ across_swizzle<T, R>(l);
+            *reinterpret_cast<uint4*>(stage + l * PER_LINE * 16 + slot * 16) = held[p];
+        }
+    }
+};
+
+template <typename T, int BM, int BN, int WGM, int WGN, class OA, class OB>
+__device__ __forceinline__ void product_of_tile(unsigned char* smem, const OA& oa, const OB& ob, int h0, int h1,
+                                                f32x16_t (&acc)[BM / WGM / 32][BN / WGN / 32]) {
+    constexpr int NT = WGM * WGN * 64, TM = BM / WGM / 32, TN = BN / WGN / 32, KSTEPS = kLineBytes / 32;
+    const int lane = threadIdx.x & 63, wv = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), wm = wv / WGN, wn = wv % WGN;
+    unsigned char *const sa = smem, *const sb = smem + BM * kLineBytes;
+#pragma unroll
+    for (int i = 0; i < TM; ++i)
+#pragma unroll
+        for (int j = 0; j < TN; ++j)
+#pragma unroll
+            for (int e = 0; e < 16; ++e) acc[i][j][e] = 0.0f;
+    if (h0 >= h1) return;
+    RegStage<T, BM, NT, OA> ra;
+    RegStage<T, BN, NT, OB> rb;
+    ra.load(oa, h0);
+    rb.load(ob, h0);
+    for (int h = h0; h < h1; ++h) {
+        __syncthreads();   // the stage before has been read
+        ra.store(sa);
+        rb.store(sb);
+        __syncthreads();
+        if (h + 1 < h1) {
+            ra.load(oa, h + 1);
+            rb.load(ob, h + 1);
+        }
+#pragma unroll
+        for (int kk = 0; kk < KSTEPS; ++kk) {
+            typename DenseFrag<T>::type a[TM], b[TN];
+#pragma unroll
+            for (int i = 0; i < TM; ++i) a[i] = FragReader<T, OA::kAlong, BM>::read(sa, wm * TM + i, kk, lane);
+#pragma unroll
+            for (int j = 0; j < TN; ++j) b[j] = FragReader<T, OB::kAlong, BN>::read(sb, wn * TN + j, kk, lane);
+#pragma unroll
+            for (int i = 0; i < TM; ++i)
+#pragma unroll
+                for (int j = 0; j < TN; ++j) dense_mma(acc[i][j], a[i], b[j]);
+        }
+    }
+    __syncthreads();
+}
+
+// ---- a tile's sums as rows: 32 rows of every wavefront row at a time pass through the LDS.  out.start(c, valid): the thread's V columns from c on, the same for all of
+// its rows, of which `valid` exist; out.row(m, valid, v): their sums in row m. ----
+template <int BM, int BN, int WGM>
+constexpr size_t rows_lds() { return (size_t)32 * WGM * (BN + 4) * 4; }
+
+template <int WGN, int TM, int TN>
+__device__ __forceinline__ void strip_to_lds(float* tile, int pitch, const f32x16_t (&acc)[TM][TN], int i) {
+    const int lane = threadIdx.x & 63, wv = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), wm = wv / WGN, wn = wv % WGN;
+#pragma unroll
+    for (int j = 0; j < TN; ++j)
+#pragma unroll
+        for (int e = 0; e < 16; ++e)
+            tile[(wm * 32 + 8 * (e >> 2) + 4 * (lane >> 5) + (e & 3)) * pitch + (wn * TN + j) * 32 + (lane & 31)] = acc[i][j][e];
+}
+
+template <int BM, int BN, int WGM, int WGN, int V, class Out>
+__device__ __forceinline__ void tile_as_rows(unsigned char* smem, const f32x16_t (&acc)[BM / WGM / 32][BN / WGN / 32], int m0, int n0, int M, int N, Out& out) {
+    constexpr int NT = WGM * WGN * 64, PITCH = BN + 4, GROUPS = BN / V, STEP = NT / GROUPS;
+    static_assert(NT % GROUPS == 0 && V % 4 == 0, "a thread keeps its columns");
+    float* const tile = reinterpret_cast<float*>(smem);
+    const int tid = threadIdx.x, c = (tid % GROUPS) * V, valid = N - n0 - c;
+    if (valid > 0) out.template start<V>(n0 + c, valid);
+#pragma unroll
+    for (int i = 0; i < BM / WGM / 32; ++i) {
+        if (i > 0) __syncthreads();
+        strip_to_lds<WGN>(tile, PITCH, acc, i);
+        __syncthreads();
+        for (int r = tid / GROUPS; r < 32 * WGM; r += STEP) {
+            const int m = m0 + (r >> 5) * (BM / WGM) + i * 32 + (r & 31);
+            if (m >= M || valid <= 0) continue;
+            float v[V];
+#pragma unroll
+            for (int q = 0; q < V; q += 4) *reinterpret_cast<f32x4_t*>(v + q) = *reinterpret_cast<const f32x4_t*>(tile + r * PITCH + c + q);
+            out.template row<V>(m, n0 + c, valid, v);
+        }
+    }
+}
+
+// The same for the two products of a gated block (PairedRows): BN / 2 columns of each; out.row(m, c, valid, first's sums, second's sums).
+template <int BM, int BN, int WGM, int WGN, int V, class Out>
+__device__ __forceinline__ void pair_as_rows(unsigned char* smem, const f32x16_t (&acc)[BM / WGM / 32][BN / WGN / 32], int m0, int n0, int M, int N, Out& out) {
+    constexpr int NT = WGM * WGN * 64, PITCH = BN + 4, GROUPS = BN / 2 / V, STEP = NT / GROUPS, HALF = BN / WGN / 2;
+    static_assert(NT % GROUPS == 0 && V % 4 == 0 && HALF % 32 == 0, "a thread keeps its columns");
+    float* const tile = reinterpret_cast<float*>(smem);
+    const int tid = threadIdx.x, c = (tid % GROUPS) * V, valid = N - n0 - c, at = c / HALF * 2 * HALF + c % HALF;
+    if (valid > 0) out.template start<V>(n0 + c, valid);
+#pragma unroll
+    for (int i = 0; i < BM / WGM / 32; ++i) {
+        if (i > 0) __syncthreads();
+        strip_to_lds<WGN>(tile, PITCH, acc, i);
+        __syncthreads();
+        for (int r = tid / GROUPS; r < 32 * WGM; r += STEP) {
+            const int m = m0 + (r >> 5) * (BM / WGM) + i * 32 + (r & 31);
+            if (m >= M || valid <= 0) continue;
+            float v[V], w[V];
+#pragma unroll
+            for (int q = 0; q < V; q += 4) {
+                *reinterpret_cast<f32x4_t*>(v + q) = *reinterpret_cast<const f32x4_t*>(tile + r * PITCH + at + q);
+                *reinterpret_cast<f32x4_t*>(w + q) = *reinterpret_cast<const f32x4_t*>(tile + r * PITCH + at + HALF + q);
+            }
+            out.template row<V>(m, n0 + c, valid, v, w);
+        }
+    }
+}
+
+// ---- values in and out ----
+__device__ __forceinline__ float to_float(float v) { return v; }
+__device__ __forceinline__ float to_float(uint16_t v) { return bf16_bits_to_float(v); }
+// (bf16: to nearest, ties to even)
+template <typename T> __device__ __forceinline__ T from_float(float v) {
+    if constexpr (sizeof(T) == 4) return v;
+    else return __builtin_bit_cast(uint16_t, (__bf16)v);
+}
+template <typename T, int V>
+__device__ __forceinline__ void store_values(T* p, const float (&v)[V], int valid) {
+    if (valid >= V) {
+        typename AnyPlace<T, V>::type w;
+#pragma unroll
+        for (int q = 0; q < V; ++q) w[q] = from_float<T>(v[q]);
+        *reinterpret_cast<typename AnyPlace<T, V>::type*>(p) = w;
+    } else {
+#pragma unroll
+        for (int q = 0; q < V; ++q)
+            if (q < valid) p[q] = from_float<T>(v[q]);
+    }
+}
+template <typename T, int V>
+__device__ __forceinline__ void load_values(const T* p, float (&v)[V], int valid) {
+    if (valid >= V) {
+        const typename AnyPlace<T, V>::type w = *reinterpret_cast<const typename AnyPlace<T, V>::type*>(p);
+#pragma unroll
+        for (int q = 0; q < V; ++q) v[q] = to_float((T)w[q]);
+    } else {
+#pragma unroll
+        for (int q = 0; q < V; ++q) v[q] = q < valid ? to_float(p[q]) : 0.0f;
+    }
+}
+
+// The activations of these products: apply_act's, and v * sigmoid(v); and their slopes.
+__device__ __forceinline__ float act_value(float v, int act) {
+    if (act == SRIGL_ACT_SILU) return v / (1.0f + expf(-v));
+    if (act == SRIGL_ACT_RELU) return v < 0.0f ? 0.0f : v;   // (what is no number stays none)
+    return apply_act(v, act);
+}
+__device__ __forceinline__ float act_slope(float v, int act) {
+    if (act == SRIGL_ACT_RELU) return v > 0.0f ? 1.0f : 0.0f;
+    if (act == SRIGL_ACT_GELU) return 0.5f * (1.0f + erff(v * 0.70710678118654752440f)) + v * expf(-0.5f * v * v) * 0.39894228040143267794f;
+    if (act == SRIGL_ACT_SILU) {
+        const float p = 1.0f / (1.0f + expf(-v));
+        return p * (1.0f + v * (1.0f - p));
+    }
+    return 1.0f;
+}
+
+// ---- kernel and launch ----
+// Sums of a part of K, [parts][M][N] (of a pair: [parts][M][2 N], the second's behind the first's)
+struct PartOut {
+    float* part;
+    int N;
+    long long pitch;
+    template <int V> __device__ void start(int, int) {}
+    template <int V> __device__ void row(int m, int c, int valid, const float (&v)[V]) { store_values<float, V>(part + (size_t)m * pitch + c, v, valid); }
+    template <int V> __device__ void row(int m, int c, int valid, const float (&v)[V], const float (&w)[V]) {
+        store_values<float, V>(part + (size_t)m * pitch + c, v, valid);
+        store_values<float, V>(part + (size_t)m * pitch + N + c, w, valid);
+    }
+};
+template <class Out, int V, bool PAIR>
+__global__ __launch_bounds__(256) void k_dense_join(const float* __restrict__ part, int parts, int M, int N, Out out) {
+    const int c = (blockIdx.x * 256 + threadIdx.x) * V, valid = N - c;
+    if (valid <= 0) return;
+    out.template start<V>(c, valid);
+    const long long pitch = PAIR ? 2ll * N : N;
+    for (int m = blockIdx.y; m < M; m += gridDim.y) {
+        float v[V] = {}, w[V] = {};
+        for (int z = 0; z < parts; ++z) {
+            const float* const p = part + ((size_t)z * M + m) * pitch + c;
+            float t[V];
+            load_values<float, V>(p, t, valid);
+#pragma unroll
+            for (int q = 0; q < V; ++q) v[q] += t[q];
+            if constexpr (PAIR) {
+                load_values<float, V>(p + N, t, valid);
+#pragma unroll
+                for (int q = 0; q < V; ++q) w[q] += t[q];
+            }
+        }
+        if constexpr (PAIR) out.template row<V>(m, c, valid, v, w);
+        else out.template row<V>(m, c, valid, v);
+    }
+}
+
+// M x N results (PAIR: of both products) of `stages` stages of K, in `parts` parts that are summed from `part` by a second launch.
+template <typename T, int BM, int BN, int WGM, int WGN, bool PAIR, class OA, class OB, class Out>
+__global__ __launch_bounds__(WGM * WGN * 64) void k_dense(OA oa, OB ob, int M, int N, int stages, int parts, Out out, float* part) {
+    extern __shared__ __attribute__((aligned(1024))) unsigned char smem[];
+    constexpr int COLS = PAIR ? BN / 2 : BN, V = kPiece<T>;
+    int tile_m, tile_n;
+    if (!tile_of_workgroup(blockIdx.x, (M + BM - 1) / BM, (N + COLS - 1) / COLS, &tile_m, &tile_n)) return;
+    const int m0 = tile_m * BM, n0 = tile_n * COLS;
+    oa.move(m0);
+    ob.move(n0);
+    const int h0 = (int)((long long)blockIdx.y * stages / parts), h1 = (int)((long long)(blockIdx.y + 1) * stages / parts);
+    f32x16_t acc[BM / WGM / 32][BN / WGN / 32];
+    product_of_tile<T, BM, BN, WGM, WGN>(smem, oa, ob, h0, h1, acc);
+    if (parts > 1) {
+        const long long pitch = PAIR ? 2ll * N : N;
+        PartOut to{part + (size_t)blockIdx.y * M * pitch, N, pitch};
+        if constexpr (PAIR) pair_as_rows<BM, BN, WGM, WGN, 4>(smem, acc, m0, n0, M, N, to);
+        else tile_as_rows<BM, BN, WGM, WGN, 4>(smem, acc, m0, n0, M, N, to);
+        return;
+    }
+    if constexpr (PAIR) pair_as_rows<BM, BN, WGM, WGN, V>(smem, acc, m0, n0, M, N, out);
+    else tile_as_rows<BM, BN, WGM, WGN, V>(smem, acc, m0, n0, M, N, out);
+}
+
+template <typename T, int BM, int BN, int WGM, int WGN, bool PAIR, class OA, class OB, class Out>
+static srigl_status launch_dense(const OA& oa, const OB& ob, int M, int N, int stages, int parts, const Out& out, float* part, hipStream_t st) {
+    constexpr size_t ring = (size_t)(BM + BN) * kLineBytes, rows = rows_lds<BM, BN, WGM>(), lds = ring > rows ? ring : rows;
+    static_assert(lds <= kLdsMax, "LDS");
+    if (M <= 0 || N <= 0) return SRIGL_OK;
+    constexpr int COLS = PAIR ? BN / 2 : BN;
+    auto kern = k_dense<T, BM, BN, WGM, WGN, PAIR, OA, OB, Out>;
+    static LdsLimit limit;
+    if (limit.ensure(kern, lds) != SRIGL_OK) return SRIGL_ERR_HIP;
+    const long long tiles = ((M + BM - 1ll) / BM) * ((N + COLS - 1ll) / COLS), n_wg = (tiles + kXcds - 1) / kXcds * kXcds;
+    if (n_wg > 0x7fffffffll || parts < 1 || parts > 65535) return SRIGL_ERR_UNSUPPORTED;
+    hipLaunchKernelGGL(kern, dim3((unsigned)n_wg, (unsigned)parts), dim3(WGM * WGN * 64), lds, st, oa, ob, M, N, stages, parts, out, part);
+    if (parts > 1) {
+        const dim3 grid((unsigned)((N + 1023ll) / 1024), (unsigned)std::min(M, 65535));
+        hipLaunchKernelGGL((k_dense_join<Out, 4, PAIR>), grid, dim3(256), 0, st, part, parts, M, N, out);
+    }
+    return hip_ok(hipGetLastError());
+}
+template <typename T> inline int stages_of(long long K) { return (int)((K + kStageK<T> - 1) / kStageK<T>); }
+
+constexpr int kMaxSide = 1 << 30;   // rows and columns of a product
+inline bool known_dtype(srigl_dtype t) { return t == SRIGL_F32 || t == SRIGL_BF16; }
+inline bool known_act(srigl_activation a) { return a == SRIGL_ACT_NONE || a == SRIGL_ACT_RELU || a == SRIGL_ACT_GELU || a == SRIGL_ACT_SILU; }
+inline size_t dtype_bytes(srigl_dtype t) { return t == SRIGL_F32 ? 4 : 2; }
+// whether some of the pointers do not stand at an element
+inline bool astray(size_t elem, std::initializer_list<const void*> ps) {
+    uintptr_t bits = 0;
+    for (const void* p : ps) bits |= reinterpret_cast<uintptr_t>(p);
+    return (bits & (elem - 1)) != 0;
+}
+
+}  // namespace srigl

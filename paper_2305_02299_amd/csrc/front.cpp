@@ -379,6 +379,204 @@ PyObject* condense(PyObject*, PyObject* const* a, Py_ssize_t n_args) {
     });
 }
 
+// ---- feed-forward blocks in the structured-only form ----
+// A tensor of these sizes and type on the current stream's device; none (null) only where `optional`.
+const at::Tensor* shaped(PyObject* o, const char* what, at::IntArrayRef size, bool optional = false) {
+    const at::Tensor* t = tensor(o);
+    if (!t) {
+        if (!optional) PyErr_Format(PyExc_TypeError, "%s: a tensor is expected", what);
+        if (!optional) throw Failed{};
+        return nullptr;
+    }
+    if (t->sizes() != size) {
+        PyErr_Format(PyExc_AssertionError, "%s has other sizes than the layer and the batch", what);
+        throw Failed{};
+    }
+    if (t->device().index() != c10::hip::getCurrentHIPStream().device_index()) {
+        PyErr_Format(PyExc_AssertionError, "%s is not on the current device", what);
+        throw Failed{};
+    }
+    return t;
+}
+void of_type(const at::Tensor* t, bool ok, const char* what) {
+    if (t && !ok) {
+        PyErr_Format(PyExc_TypeError, "%s has another element type than the call takes", what);
+        throw Failed{};
+    }
+}
+void* data(const at::Tensor* t) { return t ? t->data_ptr() : nullptr; }
+const float* floats(PyObject* o, const char* what, int64_t n) {
+    const at::Tensor* t = shaped(o, what, {n}, true);
+    of_type(t, t && t->scalar_type() == at::kFloat, what);
+    return static_cast<const float*>(data(t));
+}
+// x, and the rows of a weight matrix with x's columns; its rows are the result
+int64_t product_of(PyObject* xo, PyObject* wo, const at::Tensor*& x, const at::Tensor*& W) {
+    x = tensor(xo), W = tensor(wo);
+    if (!x || !W || x->dim() != 2 || W->dim() != 2) fail(PyExc_TypeError, "x is [batch, d_in], the weights [neurons, d_in]");
+    if (x->size(0) > INT32_MAX || x->size(1) > INT32_MAX || W->size(0) > INT32_MAX) fail(PyExc_OverflowError, "32-bit sizes are expected");
+    shaped(xo, "x", {x->size(0), x->size(1)});
+    shaped(wo, "the weight matrix", {W->size(0), x->size(1)});
+    of_type(W, dtype_of(*W) == dtype_of(*x), "the weight matrix");
+    return W->size(0);
+}
+at::Tensor workspace(size_t bytes, const at::Tensor& like) { return bytes ? fresh({(int64_t)bytes}, at::kByte, like) : at::Tensor(); }
+void* data(const at::Tensor& t) { return t.defined() ? t.data_ptr() : nullptr; }
+PyObject* wrapped(at::Tensor& t) {
+    if (!t.defined()) Py_RETURN_NONE;
+    PyObject* o = THPVariable_Wrap(std::move(t));
+    if (!o) throw Failed{};
+    return o;
+}
+// The tensors as a tuple, None for the undefined ones
+template <size_t N>
+PyObject* tuple_of(at::Tensor (&ts)[N]) {
+    PyObject* out = PyTuple_New(N);
+    if (!out) throw Failed{};
+    try {
+        for (size_t i = 0; i < N; ++i) PyTuple_SET_ITEM(out, i, wrapped(ts[i]));
+    } catch (...) {
+        Py_DECREF(out);
+        throw;
+    }
+    return out;
+}
+
+// The layer of a call: W's rows are the stored neurons
+struct LayerArgs {
+    const at::Tensor *x, *W, *active;
+    int32_t B, d_in, d_out, n;
+    const float* bias;
+    srigl_dtype type;
+    LayerArgs(PyObject* xo, PyObject* Wo, PyObject* activeo, PyObject* biaso, PyObject* d_outo) {
+        n = (int32_t)product_of(xo, Wo, x, W);
+        B = (int32_t)x->size(0), d_in = (int32_t)x->size(1), d_out = int32(d_outo), type = dtype_of(*x);
+        if (d_out < 0) fail(PyExc_ValueError, "a negative size");
+        active = shaped(activeo, "active", {n}, true);
+        of_type(active, active && active->scalar_type() == at::kInt, "active");
+        bias = floats(biaso, "bias", d_out);
+    }
+    const int32_t* list() const { return static_cast<const int32_t*>(data(active)); }
+};
+
+// structured_act(x, Wd, active, bias, d_out, residual, act, fp32, save, y) -> y, or (y, z) with save
+// y None: allocated, in fp32 or x's type; else its type says which
+PyObject* structured_act(PyObject*, PyObject* const* a, Py_ssize_t n) {
+    return guarded([&](PyObject*& out) {
+        need(n, 10);
+        const LayerArgs l(a[0], a[1], a[2], a[3], a[4]);
+        const srigl_activation act = (srigl_activation)int32(a[6]);
+        const bool save = PyObject_IsTrue(a[8]) == 1;
+        const at::Tensor* given = shaped(a[9], "y", {l.B, l.d_out}, true);
+        const srigl_dtype yt = given ? dtype_of(*given) : PyObject_IsTrue(a[7]) == 1 ? SRIGL_F32 : l.type;
+        const at::Tensor* residual = shaped(a[5], "residual", {l.B, l.d_out}, true);
+        of_type(residual, residual && dtype_of(*residual) == yt, "residual");
+        at::Tensor made[2];
+        if (!given) made[0] = fresh({l.B, l.d_out}, yt == SRIGL_F32 ? at::kFloat : l.x->scalar_type(), *l.x);
+        if (save) made[1] = fresh({l.B, l.n}, l.x->scalar_type(), *l.x);
+        void* const y = given ? given->data_ptr() : made[0].data_ptr();
+        const size_t bytes = srigl_structured_act_workspace_bytes(l.B, l.d_in, l.n, l.type);
+        const at::Tensor ws = workspace(bytes, *l.x);
+        void* st = stream();
+        srigl_status rc;
+        Py_BEGIN_ALLOW_THREADS
+        rc = srigl_structured_linear_fwd_act(data(l.x), l.type, l.B, l.d_in, data(l.W), l.type, l.list(), l.n, l.bias, data(residual), l.d_out, y, yt, data(made[1]), act,
+                                             data(ws), bytes, st);
+        Py_END_ALLOW_THREADS
+        check(rc, "srigl_structured_linear_fwd_act");
+        if (given) made[0] = *given;
+        out = save ? tuple_of(made) : wrapped(made[0]);
+    });
+}
+
+// structured_bwd(dy, x, Wd, active, bias, d_out, z, act, want) -> (dx, dWd, dbias); want: 1, 2, 4 for each, None for the others
+PyObject* structured_bwd(PyObject*, PyObject* const* a, Py_ssize_t n) {
+    return guarded([&](PyObject*& out) {
+        need(n, 9);
+        const LayerArgs l(a[1], a[2], a[3], a[4], a[5]);
+        const at::Tensor* dy = shaped(a[0], "dy", {l.B, l.d_out});
+        const at::Tensor* z = shaped(a[6], "z", {l.B, l.n}, true);
+        of_type(z, z && dtype_of(*z) == l.type, "z");
+        const srigl_activation act = (srigl_activation)int32(a[7]);
+        const int32_t want = int32(a[8]);
+        at::Tensor made[3];
+        if (want & 1) made[0] = fresh({l.B, l.d_in}, l.x->scalar_type(), *l.x);
+        if (want & 2) made[1] = fresh({l.n, l.d_in}, l.x->scalar_type(), *l.x);
+        if (want & 4) made[2] = fresh({l.d_out}, at::kFloat, *l.x);
+        const size_t bytes = srigl_structured_bwd_workspace_bytes(l.B, l.d_in, l.n, l.d_out, l.type);
+        const at::Tensor ws = workspace(bytes, *l.x);
+        const srigl_dtype dt = dtype_of(*dy);
+        void* st = stream();
+        srigl_status rc;
+        Py_BEGIN_ALLOW_THREADS
+        rc = srigl_structured_linear_bwd(data(dy), dt, data(l.x), l.type, l.B, l.d_in, data(l.W), l.type, l.list(), l.n, l.bias, data(z), l.d_out, act, data(made[0]),
+                                         data(made[1]), static_cast<float*>(data(made[2])), data(ws), bytes, st);
+        Py_END_ALLOW_THREADS
+        check(rc, "srigl_structured_linear_bwd");
+        out = tuple_of(made);
+    });
+}
+
+// gated_fwd(x, Wg, Wu, bias_g, bias_u, act, save) -> h, or (h, g, u) with save
+PyObject* gated_fwd(PyObject*, PyObject* const* a, Py_ssize_t n_args) {
+    return guarded([&](PyObject*& out) {
+        need(n_args, 7);
+        const at::Tensor *x, *Wg, *Wu;
+        const int32_t n = (int32_t)product_of(a[0], a[1], x, Wg);
+        if (product_of(a[0], a[2], x, Wu) != n) fail(PyExc_AssertionError, "both weight matrices have as many rows");
+        const float *bg = floats(a[3], "bias_g", n), *bu = floats(a[4], "bias_u", n);
+        const srigl_activation act = (srigl_activation)int32(a[5]);
+        const bool save = PyObject_IsTrue(a[6]) == 1;
+        const int32_t B = (int32_t)x->size(0), d_in = (int32_t)x->size(1);
+        at::Tensor made[3];
+        for (int i = 0; i < (save ? 3 : 1); ++i) made[i] = fresh({B, n}, x->scalar_type(), *x);
+        const srigl_dtype t = dtype_of(*x);
+        const size_t bytes = srigl_gated_workspace_bytes(B, d_in, n, t);
+        const at::Tensor ws = workspace(bytes, *x);
+        void* st = stream();
+        srigl_status rc;
+        Py_BEGIN_ALLOW_THREADS
+        rc = srigl_gated_linear_fwd(data(x), t, B, d_in, data(Wg), data(Wu), t, n, bg, bu, act, data(made[0]), data(made[1]), data(made[2]), data(ws), bytes, st);
+        Py_END_ALLOW_THREADS
+        check(rc, "srigl_gated_linear_fwd");
+        out = save ? tuple_of(made) : wrapped(made[0]);
+    });
+}
+
+// gated_bwd(dh, x, Wg, Wu, g, u, act, want) -> (dx, dWg, dWu, dbias_g, dbias_u); want: 1 dx, 2 the weights', 4 the biases'
+PyObject* gated_bwd(PyObject*, PyObject* const* a, Py_ssize_t n_args) {
+    return guarded([&](PyObject*& out) {
+        need(n_args, 8);
+        const at::Tensor *x, *Wg, *Wu;
+        const int32_t n = (int32_t)product_of(a[1], a[2], x, Wg);
+        if (product_of(a[1], a[3], x, Wu) != n) fail(PyExc_AssertionError, "both weight matrices have as many rows");
+        const int32_t B = (int32_t)x->size(0), d_in = (int32_t)x->size(1);
+        const srigl_dtype t = dtype_of(*x);
+        const at::Tensor *dh = shaped(a[0], "dh", {B, n}), *g = shaped(a[4], "g", {B, n}), *u = shaped(a[5], "u", {B, n});
+        of_type(dh, dtype_of(*dh) == t, "dh");
+        of_type(g, dtype_of(*g) == t, "g");
+        of_type(u, dtype_of(*u) == t, "u");
+        const srigl_activation act = (srigl_activation)int32(a[6]);
+        const int32_t want = int32(a[7]);
+        at::Tensor made[5];
+        if (want & 1) made[0] = fresh({B, d_in}, x->scalar_type(), *x);
+        if (want & 2)
+            for (int i = 1; i < 3; ++i) made[i] = fresh({n, d_in}, x->scalar_type(), *x);
+        if (want & 4)
+            for (int i = 3; i < 5; ++i) made[i] = fresh({n}, at::kFloat, *x);
+        const size_t bytes = srigl_gated_bwd_workspace_bytes(B, d_in, n, t);
+        const at::Tensor ws = workspace(bytes, *x);
+        void* st = stream();
+        srigl_status rc;
+        Py_BEGIN_ALLOW_THREADS
+        rc = srigl_gated_linear_bwd(data(dh), data(x), t, B, d_in, data(Wg), data(Wu), t, n, data(g), data(u), act, data(made[0]), data(made[1]), data(made[2]),
+                                    static_cast<float*>(data(made[3])), static_cast<float*>(data(made[4])), data(ws), bytes, st);
+        Py_END_ALLOW_THREADS
+        check(rc, "srigl_gated_linear_bwd");
+        out = tuple_of(made);
+    });
+}
+
 PyMethodDef methods[] = {
     {"set_error", set_error, METH_O, "the exception type of a failed call"},
     {"linear_fwd", (PyCFunction)(void (*)(void))linear_fwd, METH_FASTCALL, "srigl_condensed_linear_fwd"},
@@ -387,6 +585,10 @@ PyMethodDef methods[] = {
     {"split_bytes", (PyCFunction)(void (*)(void))split_bytes, METH_FASTCALL, "srigl_structured_split_plan"},
     {"condense", (PyCFunction)(void (*)(void))condense, METH_FASTCALL, "srigl_condense into new tensors"},
     {"mask_update", (PyCFunction)(void (*)(void))mask_update, METH_FASTCALL, "srigl_mask_update"},
+    {"structured_act", (PyCFunction)(void (*)(void))structured_act, METH_FASTCALL, "srigl_structured_linear_fwd_act"},
+    {"structured_bwd", (PyCFunction)(void (*)(void))structured_bwd, METH_FASTCALL, "srigl_structured_linear_bwd"},
+    {"gated_fwd", (PyCFunction)(void (*)(void))gated_fwd, METH_FASTCALL, "srigl_gated_linear_fwd"},
+    {"gated_bwd", (PyCFunction)(void (*)(void))gated_bwd, METH_FASTCALL, "srigl_gated_linear_bwd"},
     {nullptr, nullptr, 0, nullptr}};
 PyModuleDef module = {PyModuleDef_HEAD_INIT, "_front", "calls into libsrigl", -1, methods, nullptr, nullptr, nullptr, nullptr};
 

@@ -1,0 +1,180 @@
+// One layer in the structured-only form with bias, activation and residual behind the product, and a gated block (gfx950):
+//     z[b][s] = bias[a(s)] + sum_j Wd[s][j] x[b][j],   y[b][a(s)] = act(z[b][s]) + r[b][a(s)],   other columns c: act(bias[c]) + r[b][c]
+//     h[b][c] = act(bg[c] + sum_j Wg[c][j] x[b][j]) * (bu[c] + sum_j Wu[c][j] x[b][j])
+// The gated block is one product over both weight matrices' rows: a workgroup's tile holds the same rows of both, each wavefront the gate's sums and the
+// up-projection's of the same neurons, so that they meet in the epilogue and neither projection goes to memory (unless the caller keeps them for
+// the backward pass).
+#include "dense_tile.h"
+
+namespace srigl {
+
+template <typename T, typename TY>
+struct LinearOut {
+    const int32_t* active;
+    int n_active;
+    const float* bias;
+    const TY* residual;
+    int d_out;
+    TY* y;
+    T* z;      // pre-activations [B][n_active], or nullptr
+    int act;
+    float b[8];    // of the thread's columns
+
+    template <int V> __device__ void start(int s, int valid) {
+#pragma unroll
+        for (int q = 0; q < V; ++q) {
+            b[q] = 0.0f;
+            if (bias && q < valid) {
+                const int c = active ? active[s + q] : s + q;
+                if ((unsigned)c < (unsigned)d_out) b[q] = bias[c];
+            }
+        }
+    }
+    // the ablated columns lo .. hi - 1
+    __device__ void ablated(int m, int lo, int hi) {
+        for (int c = max(lo, 0); c < min(hi, d_out); ++c) {
+            const size_t at = (size_t)m * d_out + c;
+            const float v = act_value(bias ? bias[c] : 0.0f, act);
+            y[at] = from_float<TY>(residual ? v + to_float(residual[at]) : v);
+        }
+    }
+    template <int V> __device__ void row(int m, int s, int valid, float (&v)[V]) {
+#pragma unroll
+        for (int q = 0; q < V; ++q) v[q] += b[q];
+        if (z) store_values<T, V>(z + (size_t)m * n_active + s, v, valid);
+#pragma unroll
+        for (int q = 0; q < V; ++q) v[q] = act_value(v[q], act);
+        if (!active) {
+            const size_t at = (size_t)m * d_out + s;
+            if (residual) {
+                float r[V];
+                load_values<TY, V>(residual + at, r, valid);
+#pragma unroll
+                for (int q = 0; q < V; ++q) v[q] += r[q];
+            }
+            store_values<TY, V>(y + at, v, valid);
+            return;
+        }
+        // stored neuron s + q writes the ablated columns in front of it too, the last one those behind it
+#pragma unroll
+        for (int q = 0; q < V; ++q) {
+            if (q >= valid) break;
+            const int c = active[s + q];
+            ablated(m, s + q > 0 ? active[s + q - 1] + 1 : 0, c);
+            if ((unsigned)c < (unsigned)d_out) {
+                const size_t at = (size_t)m * d_out + c;
+                y[at] = from_float<TY>(residual ? v[q] + to_float(residual[at]) : v[q]);
+            }
+            if (s + q == n_active - 1) ablated(m, c + 1, d_out);
+        }
+    }
+};
+
+template <typename T>
+struct GatedOut {
+    const float *bias_g, *bias_u;
+    int n;
+    T *h, *g, *u;   // g and u: nullptr where the caller does not keep them
+    int act;
+    float bg[8], bu[8];
+
+    template <int V> __device__ void start(int c, int valid) {
+#pragma unroll
+        for (int q = 0; q < V; ++q) {
+            bg[q] = bias_g && q < valid ? bias_g[c + q] : 0.0f;
+            bu[q] = bias_u && q < valid ? bias_u[c + q] : 0.0f;
+        }
+    }
+    template <int V> __device__ void row(int m, int c, int valid, float (&v)[V], float (&w)[V]) {
+        const size_t at = (size_t)m * n + c;
+#pragma unroll
+        for (int q = 0; q < V; ++q) {
+            v[q] += bg[q];
+            w[q] += bu[q];
+        }
+        if (g) {
+            store_values<T, V>(g + at, v, valid);
+            store_values<T, V>(u + at, w, valid);
+        }
+#pragma unroll
+        for (int q = 0; q < V; ++q) v[q] = act_value(v[q], act) * w[q];
+        store_values<T, V>(h + at, v, valid);
+    }
+};
+
+// No stored neuron: every column is act(bias) plus the residual.
+template <typename TY>
+__global__ __launch_bounds__(256) void k_bias_rows(const float* __restrict__ bias, const TY* residual, int B, int d_out, TY* y, int act) {
+    const int c = blockIdx.x * 256 + threadIdx.x;
+    if (c >= d_out) return;
+    const float v = act_value(bias ? bias[c] : 0.0f, act);
+    for (int m = blockIdx.y; m < B; m += gridDim.y) {
+        const size_t at = (size_t)m * d_out + c;
+        y[at] = from_float<TY>(residual ? v + to_float(residual[at]) : v);
+    }
+}
+
+template <typename T, typename TY>
+static srigl_status linear_act(const void* x, int B, int d_in, const void* Wd, const int32_t* active, int n, const float* bias, const void* residual, int d_out,
+                               void* y, void* z, int act, hipStream_t st) {
+    if (n == 0) {
+        hipLaunchKernelGGL(k_bias_rows<TY>, dim3((unsigned)((d_out + 255) / 256), (unsigned)std::min(B, 65535)), dim3(256), 0, st, bias, (const TY*)residual, B, d_out,
+                           (TY*)y, act);
+        return hip_ok(hipGetLastError());
+    }
+    const RowsOf<T> a{(const T*)x, d_in, B - 1, d_in}, w{(const T*)Wd, d_in, n - 1, d_in};
+    const LinearOut<T, TY> out{n == d_out ? nullptr : active, n, bias, (const TY*)residual, d_out, (TY*)y, (T*)z, act, {}};
+    return launch_dense<T, 64, 64, 2, 2, false>(a, w, B, n, stages_of<T>(d_in), 1, out, nullptr, st);
+}
+
+template <typename T>
+static srigl_status gated(const void* x, int B, int d_in, const void* Wg, const void* Wu, int n, const float* bias_g, const float* bias_u, int act, void* h, void* g,
+                          void* u, hipStream_t st) {
+    const RowsOf<T> a{(const T*)x, d_in, B - 1, d_in};
+    const PairedRows<T, 32> w{(const T*)Wg, (const T*)Wu, d_in, n - 1, d_in};
+    const GatedOut<T> out{bias_g, bias_u, n, (T*)h, (T*)g, (T*)u, act, {}, {}};
+    return launch_dense<T, 64, 128, 2, 2, true>(a, w, B, n, stages_of<T>(d_in), 1, out, nullptr, st);
+}
+
+}  // namespace srigl
+
+using namespace srigl;
+
+extern "C" {
+
+size_t srigl_structured_act_workspace_bytes(int32_t B, int32_t d_in, int32_t n_active, srigl_dtype dtype) { return 0; }
+
+srigl_status srigl_structured_linear_fwd_act(const void* x, srigl_dtype x_dtype, int32_t B, int32_t d_in, const void* Wd, srigl_dtype w_dtype, const int32_t* active,
+                                             int32_t n_active, const float* bias, const void* residual, int32_t d_out, void* y, srigl_dtype y_dtype, void* z,
+                                             srigl_activation act, void* workspace, size_t workspace_bytes, void* stream) {
+    if (B < 0 || d_in < 0 || n_active < 0 || d_out < 0 || n_active > d_out) return SRIGL_ERR_INVALID_ARG;
+    if (!known_dtype(x_dtype) || !known_dtype(w_dtype) || !known_dtype(y_dtype) || !known_act(act)) return SRIGL_ERR_INVALID_ARG;
+    if (x_dtype != w_dtype || (y_dtype != x_dtype && y_dtype != SRIGL_F32)) return SRIGL_ERR_UNSUPPORTED;
+    if (B > kMaxSide || d_in > kMaxSide || d_out > kMaxSide) return SRIGL_ERR_UNSUPPORTED;
+    if (active == nullptr && n_active != d_out && n_active != 0) return SRIGL_ERR_INVALID_ARG;
+    if (B == 0 || d_out == 0) return SRIGL_OK;
+    if (y == nullptr || (n_active > 0 && d_in > 0 && (x == nullptr || Wd == nullptr))) return SRIGL_ERR_INVALID_ARG;
+    if (astray(dtype_bytes(x_dtype), {x, Wd, z}) || astray(dtype_bytes(y_dtype), {y, residual}) || astray(4, {bias, active})) return SRIGL_ERR_INVALID_ARG;
+    hipStream_t st = static_cast<hipStream_t>(stream);
+    if (x_dtype == SRIGL_F32) return linear_act<float, float>(x, B, d_in, Wd, active, n_active, bias, residual, d_out, y, z, act, st);
+    if (y_dtype == SRIGL_F32) return linear_act<uint16_t, float>(x, B, d_in, Wd, active, n_active, bias, residual, d_out, y, z, act, st);
+    return linear_act<uint16_t, uint16_t>(x, B, d_in, Wd, active, n_active, bias, residual, d_out, y, z, act, st);
+}
+
+size_t srigl_gated_workspace_bytes(int32_t B, int32_t d_in, int32_t n, srigl_dtype dtype) { return 0; }
+
+srigl_status srigl_gated_linear_fwd(const void* x, srigl_dtype x_dtype, int32_t B, int32_t d_in, const void* Wg, const void* Wu, srigl_dtype w_dtype, int32_t n,
+                                    const float* bias_g, const float* bias_u, srigl_activation act, void* h, void* g, void* u, void* workspace,
+                                    size_t workspace_bytes, void* stream) {
+    if (B < 0 || d_in < 0 || n < 0 || !known_dtype(x_dtype) || !known_dtype(w_dtype) || !known_act(act)) return SRIGL_ERR_INVALID_ARG;
+    if (x_dtype != w_dtype || B > kMaxSide || d_in > kMaxSide || n > kMaxSide) return SRIGL_ERR_UNSUPPORTED;
+    if ((g == nullptr) != (u == nullptr)) return SRIGL_ERR_INVALID_ARG;
+    if (B == 0 || n == 0) return SRIGL_OK;
+    if (h == nullptr || (d_in > 0 && (x == nullptr || Wg == nullptr || Wu == nullptr))) return SRIGL_ERR_INVALID_ARG;
+    if (astray(dtype_bytes(x_dtype), {x, Wg, Wu, h, g, u}) || astray(4, {bias_g, bias_u})) return SRIGL_ERR_INVALID_ARG;
+    hipStream_t st = static_cast<hipStream_t>(stream);
+    if (x_dtype == SRIGL_F32) return gated<float>(x, B, d_in, Wg, Wu, n, bias_g, bias_u, act, h, g, u, st);
+    return gated<uint16_t>(x, B, d_in, Wg, Wu, n, bias_g, bias_u, act, h, g, u, st);
+}
+
+}  // extern "C"

@@ -1,0 +1,253 @@
+// Gradients of a layer in the structured-only form and of a gated block (gfx950).
+//     layer:  dz[b][s] = dy[b][a(s)] act'(z[b][s]);  dx = dz Wd;  dWd = dz^T x;  dbias[a(s)] = sum_b dz[b][s], of ablated columns c: act'(bias[c]) sum_b dy[b][c]
+//     gated:  dg = dh u act'(g), du = dh act(g);  dx = dg Wg + du Wu;  dWg = dg^T x, dWu = du^T x;  dbias_g = sum_b dg, dbias_u = sum_b du
+// One pass over the incoming gradient writes dz (dg | du) in the storage type to the workspace and the bias gradients' partial sums, from the values before that rounding; then
+// come the two products.  The matrix units take bf16 values, so in bf16 dz is rounded once on its way into them; all sums run in fp32.
+// dz stands in the workspace with its rows padded by zeros to whole stages of K: the gated block's dg and du lie side by side, so that dx is one
+// product over both matrices' lines and the weight gradients are one product too.
+#include "dense_tile.h"
+
+namespace srigl {
+
+constexpr int kPadK = 64;   // columns dz is padded to: whole stages of either type
+static long long padded(int n) { return ((long long)n + kPadK - 1) / kPadK * kPadK; }
+
+// first place in the ascending list whose entry is >= c
+__device__ __forceinline__ int place_of(const int32_t* active, int n_active, int c) {
+    int lo = 0, hi = n_active;
+    while (lo < hi) {
+        const int mid = (lo + hi) >> 1;
+        if (active[mid] < c) lo = mid + 1;
+        else hi = mid;
+    }
+    return lo;
+}
+
+// dz[B][pitch] (pitch = padded n_active) and, per chunk of rows, the column sums of dz (ablated columns: of dy) in sums[chunk][d_out].
+template <typename T, typename TY>
+__global__ __launch_bounds__(256) void k_dz_linear(const TY* __restrict__ dy, const T* __restrict__ z, const int32_t* __restrict__ active, int n_active, int B,
+                                                  int d_out, int act, T* __restrict__ dz, int pitch, float* __restrict__ sums, int rows) {
+    const int c = blockIdx.x * 256 + threadIdx.x, m0 = blockIdx.y * rows, m1 = min(m0 + rows, B);
+    if (c >= d_out) {   // behind the last column: the padding, if the columns reach so far
+        const int s = n_active + (c - d_out);
+        if (s < pitch)
+            for (int m = m0; m < m1; ++m) dz[(size_t)m * pitch + s] = 0;
+        return;
+    }
+    int s = c;
+    bool stored = c < n_active;
+    if (active) {
+        s = place_of(active, n_active, c);
+        stored = s < n_active && active[s] == c;
+    }
+    float sum = 0.0f;
+    for (int m = m0; m < m1; ++m) {
+        float v = to_float(dy[(size_t)m * d_out + c]);
+        if (stored) {
+            if (act != SRIGL_ACT_NONE) v *= act_slope(to_float(z[(size_t)m * n_active + s]), act);
+            if (dz) dz[(size_t)m * pitch + s] = from_float<T>(v);
+        }
+        sum += v;
+    }
+    if (sums) sums[(size_t)blockIdx.y * d_out + c] = sum;
+}
+
+// (dg | du)[B][2 pitch] and the column sums of both in sums[chunk][2 n]
+template <typename T>
+__global__ __launch_bounds__(256) void k_dz_gated(const T* __restrict__ dh, const T* __restrict__ g, const T* __restrict__ u, int n, int B, int act, T* __restrict__ dz,
+                                                 int pitch, float* __restrict__ sums, int rows) {
+    const int c = blockIdx.x * 256 + threadIdx.x, m0 = blockIdx.y * rows, m1 = min(m0 + rows, B);
+    if (c >= pitch) return;
+    float sg = 0.0f, su = 0.0f;
+    for (int m = m0; m < m1; ++m) {
+        float dg = 0.0f, du = 0.0f;
+        if (c < n) {
+            const size_t at = (size_t)m * n + c;
+            const float d = to_float(dh[at]), gv = to_float(g[at]);
+            dg = d * to_float(u[at]) * act_slope(gv, act);
+            du = d * act_value(gv, act);
+        }
+        T* const to = dz + (size_t)m * 2 * pitch + c;
+        to[0] = from_float<T>(dg);
+        to[pitch] = from_float<T>(du);
+        sg += dg;
+        su += du;
+    }
+    if (sums && c < n) {
+        sums[(size_t)blockIdx.y * 2 * n + c] = sg;
+        sums[(size_t)blockIdx.y * 2 * n + n + c] = su;
+    }
+}
+
+// Bias gradients from the chunks' sums, in ascending order; columns [0, n) to first, [n, 2 n) to second (a layer: all to first, ablated columns times the slope at their bias)
+__global__ __launch_bounds__(256) void k_sum_chunks(const float* __restrict__ sums, int chunks, int cols, int n, const int32_t* __restrict__ active, int n_active,
+                                                   const float* __restrict__ bias, int act, float* __restrict__ first, float* __restrict__ second) {
+    const int c = blockIdx.x * 256 + threadIdx.x;
+    if (c >= cols) return;
+    float v = 0.0f;
+    for (int k = 0; k < chunks; ++k) v += sums[(size_t)k * cols + c];
+    if (n_active < n) {
+        const int s = active ? place_of(active, n_active, c) : 0;
+        if (!(s < n_active && active[s] == c)) v *= act_slope(bias ? bias[c] : 0.0f, act);
+    }
+    float* const to = c < n ? first : second;
+    if (to) to[c < n ? c : c - n] = v;
+}
+
+template <typename T>
+struct PlainOut {
+    T* y;
+    int N;
+    template <int V> __device__ void start(int, int) {}
+    template <int V> __device__ void row(int m, int c, int valid, float (&v)[V]) { store_values<T, V>(y + (size_t)m * N + c, v, valid); }
+};
+// Rows [0, n) to one matrix, [padded, padded + n) to a second; nullptr: not wanted
+template <typename T>
+struct TwoOut {
+    T *first, *second;
+    int N, n, padded;
+    template <int V> __device__ void start(int, int) {}
+    template <int V> __device__ void row(int m, int c, int valid, float (&v)[V]) {
+        const bool behind = m >= padded;
+        const int r = behind ? m - padded : m;
+        T* const to = behind ? second : first;
+        if (r < n && to) store_values<T, V>(to + (size_t)r * N + c, v, valid);
+    }
+};
+
+// What a backward pass takes of the workspace
+struct BwdPlan {
+    int chunk_rows, chunks;
+    size_t dz_bytes, sum_bytes, bytes;
+};
+static size_t whole(size_t bytes) { return (bytes + 255) / 256 * 256; }
+// cols: columns of dz in a row, padding included; sum_cols: of the sums
+static BwdPlan plan_bwd(int B, long long cols, long long sum_cols, size_t elem) {
+    BwdPlan p{};
+    // about a thousand workgroups of 256 columns, 8 rows to a thread at least
+    const long long groups = std::max(1ll, (sum_cols + 255) / 256), want = std::max(1ll, 1024 / groups);
+    long long rows = std::max<long long>(8, (B + want - 1) / want);
+    rows = std::max<long long>(rows, ((long long)B + 65534) / 65535);
+    p.chunk_rows = (int)std::min<long long>(rows, kMaxSide);
+    p.chunks = (int)((B + (long long)p.chunk_rows - 1) / p.chunk_rows);
+    p.dz_bytes = whole((size_t)B * cols * elem);
+    p.sum_bytes = whole((size_t)p.chunks * sum_cols * sizeof(float));
+    p.bytes = p.dz_bytes + p.sum_bytes;
+    return p;
+}
+
+template <typename T, typename TY>
+static srigl_status linear_bwd(const BwdPlan& p, const void* dy, const void* x, int B, int d_in, const void* Wd, const int32_t* active, int n, const float* bias,
+                               const void* z, int d_out, int act, void* dx, void* dWd, float* dbias, unsigned char* ws, hipStream_t st) {
+    const int pitch = (int)padded(n);
+    const int32_t* const list = n == d_out ? nullptr : active;
+    T* const dz = reinterpret_cast<T*>(ws);
+    float* const sums = reinterpret_cast<float*>(ws + p.dz_bytes);
+    if (p.chunks > 0 && (n > 0 || dbias)) {
+        const dim3 grid((unsigned)((d_out + (long long)pitch - n + 255) / 256), (unsigned)p.chunks);
+        hipLaunchKernelGGL((k_dz_linear<T, TY>), grid, dim3(256), 0, st, (const TY*)dy, (const T*)z, list, n, B, d_out, act, n > 0 ? dz : nullptr, pitch,
+                           dbias ? sums : nullptr, p.chunk_rows);
+    }
+    if (dbias) hipLaunchKernelGGL(k_sum_chunks, dim3((unsigned)((d_out + 255ll) / 256)), dim3(256), 0, st, sums, p.chunks, d_out, d_out, list, n, bias, act, dbias, nullptr);
+    srigl_status rc = hip_ok(hipGetLastError());
+    if (rc == SRIGL_OK && dx) {
+        const RowsOf<T> a{dz, pitch, B - 1, pitch};
+        const ColsOf<T> w{(const T*)Wd, d_in, d_in, n};
+        rc = launch_dense<T, 64, 64, 2, 2, false>(a, w, B, d_in, stages_of<T>(n), 1, PlainOut<T>{(T*)dx, d_in}, nullptr, st);
+    }
+    if (rc == SRIGL_OK && dWd) {
+        const ColsOf<T> a{dz, pitch, pitch, B}, b{(const T*)x, d_in, d_in, B};
+        rc = launch_dense<T, 64, 64, 2, 2, false>(a, b, n, d_in, stages_of<T>(B), 1, PlainOut<T>{(T*)dWd, d_in}, nullptr, st);
+    }
+    return rc;
+}
+
+template <typename T>
+static srigl_status gated_bwd(const BwdPlan& p, const void* dh, const void* x, int B, int d_in, const void* Wg, const void* Wu, int n, const void* g, const void* u,
+                              int act, void* dx, void* dWg, void* dWu, float* dbias_g, float* dbias_u, unsigned char* ws, hipStream_t st) {
+    const int pitch = (int)padded(n);
+    T* const dz = reinterpret_cast<T*>(ws);
+    float* const sums = reinterpret_cast<float*>(ws + p.dz_bytes);
+    const bool want_sums = dbias_g || dbias_u;
+    if (p.chunks > 0 && n > 0)
+        hipLaunchKernelGGL(k_dz_gated<T>, dim3((unsigned)((pitch + 255) / 256), (unsigned)p.chunks), dim3(256), 0, st, (const T*)dh, (const T*)g, (const T*)u, n, B, act, dz,
+                           pitch, want_sums ? sums : nullptr, p.chunk_rows);
+    if (want_sums && n > 0)
+        hipLaunchKernelGGL(k_sum_chunks, dim3((unsigned)((2ll * n + 255) / 256)), dim3(256), 0, st, sums, p.chunks, 2 * n, n, nullptr, n, nullptr, act, dbias_g, dbias_u);
+    srigl_status rc = hip_ok(hipGetLastError());
+    if (rc == SRIGL_OK && dx) {
+        const RowsOf<T> a{dz, 2ll * pitch, B - 1, 2 * pitch};
+        const PairedCols<T> w{(const T*)Wg, (const T*)Wu, d_in, d_in, n, pitch};
+        rc = launch_dense<T, 64, 64, 2, 2, false>(a, w, B, d_in, stages_of<T>(2ll * pitch), 1, PlainOut<T>{(T*)dx, d_in}, nullptr, st);
+    }
+    if (rc == SRIGL_OK && (dWg || dWu) && n > 0) {
+        const ColsOf<T> a{dz, 2ll * pitch, 2 * pitch, B}, b{(const T*)x, d_in, d_in, B};
+        rc = launch_dense<T, 64, 64, 2, 2, false>(a, b, 2 * pitch, d_in, stages_of<T>(B), 1, TwoOut<T>{(T*)dWg, (T*)dWu, d_in, n, pitch}, nullptr, st);
+    }
+    return rc;
+}
+
+static bool bwd_sizes_fit(int B, int d_in, int d_out) { return B <= kMaxSide && d_in <= kMaxSide && d_out <= kMaxSide / 2; }
+
+}  // namespace srigl
+
+using namespace srigl;
+
+extern "C" {
+
+size_t srigl_structured_bwd_workspace_bytes(int32_t B, int32_t d_in, int32_t n_active, int32_t d_out, srigl_dtype dtype) {
+    if (B < 0 || d_in < 0 || n_active < 0 || d_out < n_active || !known_dtype(dtype) || !bwd_sizes_fit(B, d_in, d_out)) return 0;
+    return plan_bwd(B, padded(n_active), d_out, dtype_bytes(dtype)).bytes;
+}
+
+srigl_status srigl_structured_linear_bwd(const void* dy, srigl_dtype dy_dtype, const void* x, srigl_dtype x_dtype, int32_t B, int32_t d_in, const void* Wd,
+                                         srigl_dtype w_dtype, const int32_t* active, int32_t n_active, const float* bias, const void* z, int32_t d_out,
+                                         srigl_activation act, void* dx, void* dWd, float* dbias, void* workspace, size_t workspace_bytes, void* stream) {
+    if (B < 0 || d_in < 0 || n_active < 0 || d_out < 0 || n_active > d_out) return SRIGL_ERR_INVALID_ARG;
+    if (!known_dtype(dy_dtype) || !known_dtype(x_dtype) || !known_dtype(w_dtype) || !known_act(act)) return SRIGL_ERR_INVALID_ARG;
+    if (x_dtype != w_dtype || (dy_dtype != x_dtype && dy_dtype != SRIGL_F32) || !bwd_sizes_fit(B, d_in, d_out)) return SRIGL_ERR_UNSUPPORTED;
+    if (active == nullptr && n_active != d_out && n_active != 0) return SRIGL_ERR_INVALID_ARG;
+    const bool rows = B > 0 && n_active > 0;   // there is a product
+    if (B > 0 && d_out > 0 && dy == nullptr && (dx || dWd || dbias)) return SRIGL_ERR_INVALID_ARG;
+    if (rows && d_in > 0 && ((dx && Wd == nullptr) || (dWd && x == nullptr))) return SRIGL_ERR_INVALID_ARG;
+    if (rows && act != SRIGL_ACT_NONE && z == nullptr && (dx || dWd || dbias)) return SRIGL_ERR_INVALID_ARG;
+    if (astray(dtype_bytes(x_dtype), {x, Wd, z, dx, dWd}) || astray(dtype_bytes(dy_dtype), {dy}) || astray(4, {bias, active, dbias})) return SRIGL_ERR_INVALID_ARG;
+    if (!dx && !dWd && !dbias) return SRIGL_OK;
+    const BwdPlan p = plan_bwd(B, padded(n_active), d_out, dtype_bytes(x_dtype));
+    if (p.bytes > 0 && workspace == nullptr) return SRIGL_ERR_CAPACITY;
+    if (workspace_bytes < p.bytes) return SRIGL_ERR_CAPACITY;
+    if ((reinterpret_cast<uintptr_t>(workspace) & 15) != 0) return SRIGL_ERR_INVALID_ARG;
+    hipStream_t st = static_cast<hipStream_t>(stream);
+    unsigned char* const ws = static_cast<unsigned char*>(workspace);
+    if (d_in == 0) dx = dWd = nullptr;
+    if (x_dtype == SRIGL_F32) return linear_bwd<float, float>(p, dy, x, B, d_in, Wd, active, n_active, bias, z, d_out, act, dx, dWd, dbias, ws, st);
+    if (dy_dtype == SRIGL_F32) return linear_bwd<uint16_t, float>(p, dy, x, B, d_in, Wd, active, n_active, bias, z, d_out, act, dx, dWd, dbias, ws, st);
+    return linear_bwd<uint16_t, uint16_t>(p, dy, x, B, d_in, Wd, active, n_active, bias, z, d_out, act, dx, dWd, dbias, ws, st);
+}
+
+size_t srigl_gated_bwd_workspace_bytes(int32_t B, int32_t d_in, int32_t n, srigl_dtype dtype) {
+    if (B < 0 || d_in < 0 || n < 0 || !known_dtype(dtype) || !bwd_sizes_fit(B, d_in, n)) return 0;
+    return plan_bwd(B, 2 * padded(n), 2ll * n, dtype_bytes(dtype)).bytes;
+}
+
+srigl_status srigl_gated_linear_bwd(const void* dh, const void* x, srigl_dtype x_dtype, int32_t B, int32_t d_in, const void* Wg, const void* Wu, srigl_dtype w_dtype,
+                                    int32_t n, const void* g, const void* u, srigl_activation act, void* dx, void* dWg, void* dWu, float* dbias_g, float* dbias_u,
+                                    void* workspace, size_t workspace_bytes, void* stream) {
+    if (B < 0 || d_in < 0 || n < 0 || !known_dtype(x_dtype) || !known_dtype(w_dtype) || !known_act(act)) return SRIGL_ERR_INVALID_ARG;
+    if (x_dtype != w_dtype || !bwd_sizes_fit(B, d_in, n)) return SRIGL_ERR_UNSUPPORTED;
+    const bool any = dx || dWg || dWu || dbias_g || dbias_u, rows = B > 0 && n > 0;
+    if (any && rows && (dh == nullptr || g == nullptr || u == nullptr)) return SRIGL_ERR_INVALID_ARG;
+    if (rows && d_in > 0 && ((dx && (Wg == nullptr || Wu == nullptr)) || ((dWg || dWu) && x == nullptr))) return SRIGL_ERR_INVALID_ARG;
+    if (astray(dtype_bytes(x_dtype), {dh, x, Wg, Wu, g, u, dx, dWg, dWu}) || astray(4, {dbias_g, dbias_u})) return SRIGL_ERR_INVALID_ARG;
+    if (!any) return SRIGL_OK;
+    const BwdPlan p = plan_bwd(B, 2 * padded(n), 2ll * n, dtype_bytes(x_dtype));
+    if (workspace_bytes < p.bytes || (p.bytes > 0 && workspace == nullptr)) return SRIGL_ERR_CAPACITY;
+    if ((reinterpret_cast<uintptr_t>(workspace) & 15) != 0) return SRIGL_ERR_INVALID_ARG;
+    hipStream_t st = static_cast<hipStream_t>(stream);
+    unsigned char* const ws = static_cast<unsigned char*>(workspace);
+    if (d_in == 0) dx = dWg = dWu = nullptr;
+    if (x_dtype == SRIGL_F32) return gated_bwd<float>(p, dh, x, B, d_in, Wg, Wu, n, g, u, act, dx, dWg, dWu, dbias_g, dbias_u, ws, st);
+    return gated_bwd<uint16_t>(p, dh, x, B, d_in, Wg, Wu, n, g, u, act, dx, dWg, dWu, dbias_g, dbias_u, ws, st);
+}
+
+}  // extern "C"

@@ -57,6 +57,10 @@ class CondensedLinear:
             B_.srigl_densify(self.W_c, self.idx if self.idx_wide is None else self.idx_wide, self.n_active, self.K, self.d_in, self.Wd)
         return self.Wd
 
+    def structured(self) -> "StructuredLinear":
+        """The layer as dense rows of its stored neurons (dense_rows(), a copy), with activation, residual and gradients."""
+        return StructuredLinear(self.d_in, self.d_out, self.dense_rows()[:self.n_active], self.active, self.bias)
+
     def choose(self, batch: int) -> int:
         return B_.srigl_choose_representation(batch, self.d_in, self.n_active, self.K, self.d_out, B_._dtype_code(self.W_c))[0]
 
@@ -154,3 +158,79 @@ def fold_mlp(layer1: CondensedLinear, layer2: CondensedLinear, act: int) -> Cond
         B_.srigl_pack_terms(W_f, idx_f, layer2.n_active, layer2.K, n1p, packed2)
     second = CondensedLinear(n1p, layer2.d_out, layer2.K, layer2.n_active, W_f, idx_f, layer2.active, bias_f, seg, packed=packed2)
     return CondensedMLP(first, second, act)
+
+
+@dataclass
+class StructuredLinear:
+    """One layer in the structured-only form on the GPU: Wd [n_active, d_in] (fp32 or bf16 storage) are the rows of the neurons that are not ablated,
+    active [n_active] int32 their columns of the result (None: every neuron is stored), bias [d_out] fp32 or None.  Forward with activation and residual, and
+    the gradients; dWd of a layer without ablated neurons in fp32 is the gradient that srigl_mask_update ranks.  Results and scratch come from torch's
+    allocator, in the order of the current stream; no autograd graph is kept."""
+
+    d_in: int
+    d_out: int
+    Wd: torch.Tensor
+    active: torch.Tensor | None = None
+    bias: torch.Tensor | None = None
+
+    def forward(self, x: torch.Tensor, act: int = B_.ACT_NONE, residual: torch.Tensor | None = None, out_dtype: torch.dtype | None = None,
+                save: bool = False, y: torch.Tensor | None = None):
+        """act(x Wd^T + bias) + residual, [batch, d_out]; out_dtype: x's (default) or fp32, and the residual's; y: where to put it (may be the residual).
+        save: returns (y, z), z the pre-activations [batch, n_active] that backward takes."""
+        assert x.dim() == 2 and x.shape[1] == self.d_in, "x is [batch, d_in]"
+        assert out_dtype in (None, x.dtype, torch.float32), "the result is of x's type or fp32"
+        return _front.structured_act(x, self.Wd, self.active, self.bias, self.d_out, residual, act, out_dtype == torch.float32, save, y)
+
+    def backward(self, dy: torch.Tensor, x: torch.Tensor, z: torch.Tensor | None = None, act: int = B_.ACT_NONE, need_dx: bool = True):
+        """(dx, dWd, dbias) for dy [batch, d_out], the gradient of forward's result (and so of the residual); z as forward saved it (None without an activation).
+        dx is None without need_dx, dbias for a layer without a bias."""
+        assert x.dim() == 2 and x.shape[1] == self.d_in, "x is [batch, d_in]"
+        return _front.structured_bwd(dy, x, self.Wd, self.active, self.bias, self.d_out, z, act, 2 + need_dx + 4 * (self.bias is not None))
+
+
+@dataclass
+class GatedLinear:
+    """The gated half of a feed-forward block on the GPU: act(x Wg^T + bias_g) * (x Wu^T + bias_u), [batch, n], in one launch.  Wg, Wu [n, d_in]: the rows of
+    the hidden neurons that are not ablated; biases [n] fp32 or None."""
+
+    d_in: int
+    n: int
+    Wg: torch.Tensor
+    Wu: torch.Tensor
+    bias_g: torch.Tensor | None = None
+    bias_u: torch.Tensor | None = None
+    act: int = B_.ACT_SILU
+
+    def forward(self, x: torch.Tensor, save: bool = False):
+        """h, or with save (h, g, u): both projections, which backward takes."""
+        assert x.dim() == 2 and x.shape[1] == self.d_in and self.Wg.shape[0] == self.n, "x is [batch, d_in], Wg [n, d_in]"
+        return _front.gated_fwd(x, self.Wg, self.Wu, self.bias_g, self.bias_u, self.act, save)
+
+    def backward(self, dh: torch.Tensor, x: torch.Tensor, g: torch.Tensor, u: torch.Tensor, need_dx: bool = True):
+        """(dx, dWg, dWu, dbias_g, dbias_u) for dh [batch, n]; dx is None without need_dx, a bias's gradient without that bias."""
+        assert x.dim() == 2 and x.shape[1] == self.d_in and self.Wg.shape[0] == self.n, "x is [batch, d_in], Wg [n, d_in]"
+        biased = self.bias_g is not None or self.bias_u is not None
+        dx, dWg, dWu, dbg, dbu = _front.gated_bwd(dh, x, self.Wg, self.Wu, g, u, self.act, 2 + need_dx + 4 * biased)
+        return dx, dWg, dWu, dbg if self.bias_g is not None else None, dbu if self.bias_u is not None else None
+
+
+@dataclass
+class GatedMLP:
+    """A gated feed-forward block: y = down(gated(x)) + residual, the down-projection's columns those of the hidden neurons that are stored."""
+
+    gated: GatedLinear
+    down: StructuredLinear   # d_in == gated.n
+
+    def forward(self, x: torch.Tensor, residual: torch.Tensor | None = None, out_dtype: torch.dtype | None = None, save: bool = False):
+        """y, or with save (y, (h, g, u)): what backward takes."""
+        if not save:
+            return self.down.forward(self.gated.forward(x), residual=residual, out_dtype=out_dtype)
+        h, g, u = self.gated.forward(x, save=True)
+        return self.down.forward(h, residual=residual, out_dtype=out_dtype), (h, g, u)
+
+    def backward(self, dy: torch.Tensor, x: torch.Tensor, saved, need_dx: bool = True):
+        """(dx, (dWg, dWu, dbias_g, dbias_u), (dWd, dbias)); the residual's gradient is dy."""
+        h, g, u = saved
+        dh, dWd, dbias = self.down.backward(dy, h)
+        dx, *projections = self.gated.backward(dh, x, g, u, need_dx)
+        return dx, tuple(projections), (dWd, dbias)
