@@ -33,10 +33,20 @@ constexpr int kLineBytes = 128;                                              // 
 template <typename T> constexpr int kStageK = kLineBytes / (int)sizeof(T);   // its elements
 template <typename T> constexpr int kPiece = 16 / (int)sizeof(T);            // elements of a 16-byte piece
 
+// From one matrix to another, in bytes
+inline long long bytes_between(const void* a, const void* b) { return (long long)(reinterpret_cast<intptr_t>(b) - reinterpret_cast<intptr_t>(a)); }
+// Whether 16-byte loads can take an operand whose rows are `pitch` apart, and a lane's 32 bits the offsets of `lines` of them
+template <typename T> inline bool direct_rows(const T* base, long long pitch, int lines) {
+    return (reinterpret_cast<uintptr_t>(base) & 15) == 0 && pitch * (long long)sizeof(T) % 16 == 0 && lines * pitch * (long long)sizeof(T) < (1ll << 31);
+}
+
 // Loads and stores of V consecutive elements from any element's address
 template <typename T, int V> struct AnyPlace { typedef T type __attribute__((ext_vector_type(V), aligned(sizeof(T)))); };
 
-// ---- operands: line(l, first, valid) is where elements first .. of line l begin, *valid how many of them there are (<= 0: none) ----
+// ---- operands ----
+// line(l, first, valid): where elements first .. of line l begin, *valid how many of them there are (<= 0: none).
+// For loads that go straight into the LDS, of operands whose lines begin at and are multiples of 16 bytes: stage(h, l) is the scalar address that lane_offset(l, first) bytes are
+// added to (l: any line of the 1 KB that the wavefront's load fills, whose lines are of one matrix), with lines and columns past the last one at the last one; past(h, l, first): behind the end of K.
 // Along K: line = tile row, elements = k.
 template <typename T> struct RowsOf {
     static constexpr bool kAlong = true;
@@ -45,20 +55,34 @@ template <typename T> struct RowsOf {
     int last, K;        // last row that there is, counted from the tile's first
     __device__ void move(int first) { base += (size_t)first * pitch; last -= first; }
     __device__ const T* line(int l, int first, int* valid) const { *valid = K - first; return base + (size_t)min(l, last) * pitch + first; }
+    __device__ const unsigned char* stage(int h, int) const { return reinterpret_cast<const unsigned char*>(base) + (size_t)h * kLineBytes; }
+    __device__ uint32_t lane_offset(int l, int first) const { return ((uint32_t)min(l, last) * (uint32_t)pitch + first) * (uint32_t)sizeof(T); }
+    __device__ bool past(int h, int, int first) const { return h * kStageK<T> + first >= K; }
+    bool direct(int lines) const { return direct_rows(base, pitch, lines) && K % kPiece<T> == 0; }
+    bool ragged() const { return K % kStageK<T> != 0; }
 };
 // The weight rows of two matrices that a gated block multiplies with, next to each other in each wavefront's part of the tile: HALF rows of the first,
 // the same HALF rows of the second.
 template <typename T, int HALF> struct PairedRows {
     static constexpr bool kAlong = true;
-    const T *base, *second;
+    const T* base;
+    long long to_second;   // bytes (a choice between two pointers of a struct went through scratch memory)
     long long pitch;
     int last, K;
-    __device__ void move(int first) { base += (size_t)first * pitch; second += (size_t)first * pitch; last -= first; }
+    __device__ void move(int first) { base += (size_t)first * pitch; last -= first; }
+    __device__ const unsigned char* of(bool second) const { return reinterpret_cast<const unsigned char*>(base) + (second ? to_second : 0); }
     __device__ const T* line(int l, int first, int* valid) const {
         const int part = l / HALF, r = (part >> 1) * HALF + l % HALF;
         *valid = K - first;
-        return ((part & 1) ? second : base) + (size_t)min(r, last) * pitch + first;
+        return reinterpret_cast<const T*>(of(part & 1)) + (size_t)min(r, last) * pitch + first;
     }
+    __device__ const unsigned char* stage(int h, int l) const { return of(l / HALF & 1) + (size_t)h * kLineBytes; }
+    __device__ uint32_t lane_offset(int l, int first) const {
+        return ((uint32_t)min((l / HALF >> 1) * HALF + l % HALF, last) * (uint32_t)pitch + first) * (uint32_t)sizeof(T);
+    }
+    __device__ bool past(int h, int, int first) const { return h * kStageK<T> + first >= K; }
+    bool direct(int lines) const { return direct_rows(base, pitch, lines) && to_second % 16 == 0 && K % kPiece<T> == 0; }
+    bool ragged() const { return K % kStageK<T> != 0; }
 };
 // Across K: line = k, elements = tile columns.
 template <typename T> struct ColsOf {
@@ -68,20 +92,38 @@ template <typename T> struct ColsOf {
     int cols, K;        // columns from there on
     __device__ void move(int first) { base += first; cols -= first; }
     __device__ const T* line(int l, int first, int* valid) const { *valid = l < K ? cols - first : 0; return base + (size_t)l * pitch + first; }
+    __device__ const unsigned char* stage(int h, int) const { return reinterpret_cast<const unsigned char*>(base + (size_t)h * kStageK<T> * pitch); }
+    __device__ uint32_t lane_offset(int l, int first) const { return ((uint32_t)l * (uint32_t)pitch + min(first, cols - kPiece<T>)) * (uint32_t)sizeof(T); }
+    __device__ bool past(int h, int l, int) const { return h * kStageK<T> + l >= K; }
+    bool direct(int) const { return direct_rows(base, pitch, kStageK<T>) && cols % kPiece<T> == 0; }
+    bool ragged() const { return K % kStageK<T> != 0; }
 };
 // Lines 0 .. n - 1 of one matrix, then, from line `padded` on, those of a second.
 template <typename T> struct PairedCols {
     static constexpr bool kAlong = false;
-    const T *base, *second;
+    const T* base;
+    long long to_second;   // bytes
     long long pitch;
     int cols, n, padded;
-    __device__ void move(int first) { base += first; second += first; cols -= first; }
+    __device__ void move(int first) { base += first; cols -= first; }
+    __device__ const T* of(bool second) const { return reinterpret_cast<const T*>(reinterpret_cast<const unsigned char*>(base) + (second ? to_second : 0)); }
     __device__ const T* line(int l, int first, int* valid) const {
         const bool behind = l >= padded;
         const int r = behind ? l - padded : l;
         *valid = r < n ? cols - first : 0;
-        return (behind ? second : base) + (size_t)r * pitch + first;
+        return of(behind) + (size_t)r * pitch + first;
     }
+    __device__ const unsigned char* stage(int h, int) const {   // (`padded` is a whole number of stages)
+        const int in_first = padded / kStageK<T>;
+        return reinterpret_cast<const unsigned char*>(of(h >= in_first) + (size_t)(h >= in_first ? h - in_first : h) * kStageK<T> * pitch);
+    }
+    __device__ uint32_t lane_offset(int l, int first) const { return ((uint32_t)l * (uint32_t)pitch + min(first, cols - kPiece<T>)) * (uint32_t)sizeof(T); }
+    __device__ bool past(int h, int l, int) const {
+        const int k = h * kStageK<T> + l;
+        return (k >= padded ? k - padded : k) >= n;
+    }
+    bool direct(int) const { return direct_rows(base, pitch, kStageK<T>) && to_second % 16 == 0 && cols % kPiece<T> == 0; }
+    bool ragged() const { return n != padded; }
 };
 
 // 16 bytes from there, zeros behind the valid elements
@@ -109,34 +151,48 @@ __device__ __forceinline__ int across_swizzle(int k) {
     else return R >= 128 ? (k & 3) << 2 : ((k >> 1) & 1) << 2;
 }
 
-// Byte offset, in a stage of R rows at 0, of what lane l reads for step kk of the 32-row block at row 0; other blocks: + block_offset.
-template <typename T, bool ALONG, int R>
+// (restrict: without it the compiler holds the read back until every load on its way into the LDS has landed, the stages ahead included; the waits for this stage are the loop's own)
+__device__ __forceinline__ s16x4_t read_across(const unsigned char* __restrict__ at) {
+    return __builtin_amdgcn_ds_read_tr16_b64_v4i16((__attribute__((address_space(3))) s16x4_t*)at);
+}
+
+// Reads a lane's fragments of the TB 32-row blocks from block `first` on, in a stage of R rows.
+template <typename T, bool ALONG, int R, int TB>
 struct FragReader {
     using F = typename DenseFrag<T>::type;
-    static constexpr int PITCH = R * (int)sizeof(T);
-    __device__ static F read(const unsigned char* stage, int block, int kk, int lane) {
+    static constexpr int PITCH = R * (int)sizeof(T), KSTEPS = kLineBytes / 32;
+    uint32_t at[ALONG ? KSTEPS : TB];   // a lane's byte offset by step (blocks are 32 * 128 bytes apart), or by block (steps are whole lines apart)
+    __device__ __forceinline__ void init(int first, int lane) {
         const int half = lane >> 5, r = lane & 31;
         if constexpr (ALONG) {
-            const int row = block * 32 + r;
-            return *reinterpret_cast<const F*>(stage + row * kLineBytes + (((2 * kk + half) ^ ((row >> 1) & 7)) << 4));
+#pragma unroll
+            for (int kk = 0; kk < KSTEPS; ++kk) at[kk] = (first * 32 + r) * kLineBytes + (((2 * kk + half) ^ ((r >> 1) & 7)) << 4);
+        } else {
+#pragma unroll
+            for (int b = 0; b < TB; ++b) {
+                if constexpr (sizeof(T) == 4) {
+                    const int c = (first + b) * 32 + r;
+                    at[b] = 4 * half * PITCH + ((((c >> 2) ^ across_swizzle<T, R>(4 * half)) << 4) | ((c & 3) << 2));
+                } else {
+                    const int i = lane & 15, c = (first + b) * 32 + (lane & 16) + 4 * (i & 3);
+                    at[b] = (8 * half + (i >> 2)) * PITCH + ((((c >> 3) ^ across_swizzle<T, R>(i >> 2)) << 4) | ((c & 4) << 1));
+                }
+            }
+        }
+    }
+    __device__ __forceinline__ F read(const unsigned char* stage, int b, int kk) const {
+        if constexpr (ALONG) {
+            return *reinterpret_cast<const F*>(stage + at[kk] + b * 32 * kLineBytes);
         } else if constexpr (sizeof(T) == 4) {
             F f;
-            const int c = block * 32 + r;
 #pragma unroll
-            for (int j = 0; j < 4; ++j) {
-                const int k = 8 * kk + 4 * half + j;
-                f[j] = *reinterpret_cast<const float*>(stage + k * PITCH + ((((c >> 2) ^ across_swizzle<T, R>(k)) << 4) | ((c & 3) << 2)));
-            }
+            for (int j = 0; j < 4; ++j) f[j] = *reinterpret_cast<const float*>(stage + at[b] + (8 * kk + j) * PITCH);
             return f;
         } else {
-            const int i = lane & 15, c = block * 32 + (lane & 16) + 4 * (i & 3);
             union { s16x4_t part[2]; F f; } u;
 #pragma unroll
-            for (int s = 0; s < 2; ++s) {
-                const int k = 16 * kk + 8 * half + 4 * s + (i >> 2);
-                const unsigned char* at = stage + k * PITCH + ((((c >> 3) ^ across_swizzle<T, R>(k)) << 4) | ((c & 4) << 1));
-                u.part[s] = __builtin_amdgcn_ds_read_tr16_b64_v4i16((__attribute__((address_space(3))) s16x4_t*)at);
-            }
+            for (int s = 0; s < 2; ++s)
+                u.part[s] = read_across(stage + at[b] + (16 * kk + 4 * s) * PITCH);
             return u.f;
         }
     }
@@ -180,6 +236,10 @@ __device__ __forceinline__ void product_of_tile(unsigned char* smem, const OA& o
 #pragma unroll
             for (int e = 0; e < 16; ++e) acc[i][j][e] = 0.0f;
     if (h0 >= h1) return;
+    FragReader<T, OA::kAlong, BM, TM> fa;
+    FragReader<T, OB::kAlong, BN, TN> fb;
+    fa.init(wm * TM, lane);
+    fb.init(wn * TN, lane);
     RegStage<T, BM, NT, OA> ra;
     RegStage<T, BN, NT, OB> rb;
     ra.load(oa, h0);
@@ -197,15 +257,140 @@ __device__ __forceinline__ void product_of_tile(unsigned char* smem, const OA& o
         for (int kk = 0; kk < KSTEPS; ++kk) {
             typename DenseFrag<T>::type a[TM], b[TN];
 #pragma unroll
-            for (int i = 0; i < TM; ++i) a[i] = FragReader<T, OA::kAlong, BM>::read(sa, wm * TM + i, kk, lane);
+            for (int i = 0; i < TM; ++i) a[i] = fa.read(sa, i, kk);
 #pragma unroll
-            for (int j = 0; j < TN; ++j) b[j] = FragReader<T, OB::kAlong, BN>::read(sb, wn * TN + j, kk, lane);
+            for (int j = 0; j < TN; ++j) b[j] = fb.read(sb, j, kk);
 #pragma unroll
             for (int i = 0; i < TM; ++i)
 #pragma unroll
                 for (int j = 0; j < TN; ++j) dense_mma(acc[i][j], a[i], b[j]);
         }
     }
+    __syncthreads();
+}
+
+// ---- the product of a tile, staged by loads straight into the LDS (operands that are direct()): a ring of NS stages.
+// Schedule of a stage (KSTEPS MFMA steps): the fragments of the next step are requested between the multiplications of a step.  Before the last step the wavefront waits until its own
+// loads of the next stage have landed and its reads of this one have returned, and meets the others at the barrier: the next stage is then complete and this one's slot free.  Behind it the first
+// fragments of the next stage are requested and, between the multiplications of this step and the next one, the pieces of stage h + NS.  A stage index past the last one requests the last one again, into a
+// slot nobody reads: the number of loads in flight at each wait is fixed. ----
+template <typename T, int R, int FIRST, int NWAVES, class Op>
+struct DirectStage {
+    static constexpr int PASSES = R * kLineBytes / 1024 / NWAVES, PER_LINE = Op::kAlong ? 8 : R / kPiece<T>;
+    static_assert(R * kLineBytes % (1024 * NWAVES) == 0, "1 KB to a wavefront's load");
+    uint32_t at[PASSES];
+    __device__ __forceinline__ static void place(int p, int wv, int lane, int* l, int* first) {
+        const int u = (p * NWAVES + wv) * 64 + lane;
+        *l = u / PER_LINE;
+        *first = ((u % PER_LINE) ^ (Op::kAlong ? (*l >> 1) & 7 : across_swizzle<T, R>(*l))) * kPiece<T>;
+    }
+    __device__ __forceinline__ void init(const Op& op, int wv, int lane) {
+#pragma unroll
+        for (int p = 0; p < PASSES; ++p) {
+            int l, first;
+            place(p, wv, lane, &l, &first);
+            at[p] = op.lane_offset(l, first);
+        }
+    }
+    template <bool RAGGED>
+    __device__ __forceinline__ void issue(const Op& op, int p, int h, unsigned char* stage, int wv, int lane) const {
+        uint32_t off = at[p];
+        asm("" : "+v"(off));   // (a lane offset from a scalar base: seen to be 32 bits only next to the load)
+        const unsigned char* g = op.stage(h, (p * NWAVES + wv) * 64 / PER_LINE) + off;
+        if (RAGGED) {
+            int l, first;
+            place(p, wv, lane, &l, &first);
+            if (op.past(h, l, first)) g = reinterpret_cast<const unsigned char*>(&g_zero16);
+        }
+        __builtin_amdgcn_global_load_lds((gptr_t)g, (lptr_t)(stage + FIRST + 1024 * (p * NWAVES + wv)), 16, 0, 0);
+    }
+};
+
+template <typename T, int BM, int BN, int WGM, int WGN, int NS, bool RAGGED, class OA, class OB>
+__device__ __forceinline__ void direct_product_of_tile(unsigned char* smem, const OA& oa, const OB& ob, int h0, int h1, f32x16_t (&acc)[BM / WGM / 32][BN / WGN / 32]) {
+    constexpr int NWAVES = WGM * WGN, TM = BM / WGM / 32, TN = BN / WGN / 32, KSTEPS = kLineBytes / 32, STAGE = (BM + BN) * kLineBytes;
+    using SA = DirectStage<T, BM, 0, NWAVES, OA>;
+    using SB = DirectStage<T, BN, BM * kLineBytes, NWAVES, OB>;
+    constexpr int PASSES = SA::PASSES + SB::PASSES;
+    static_assert(NS >= 2 && (NS - 1) * PASSES <= 63, "vmcnt range");
+    const int lane = threadIdx.x & 63, wv = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), wm = wv / WGN, wn = wv % WGN, n_st = h1 - h0;
+#pragma unroll
+    for (int i = 0; i < TM; ++i)
+#pragma unroll
+        for (int j = 0; j < TN; ++j)
+#pragma unroll
+            for (int e = 0; e < 16; ++e) acc[i][j][e] = 0.0f;
+    if (n_st <= 0) return;
+    SA la;
+    SB lb;
+    la.init(oa, wv, lane);
+    lb.init(ob, wv, lane);
+    auto issue_piece = [&](int p, int h_unclamped, int slot) {
+        const int h = h0 + min(h_unclamped, n_st - 1);
+        if (p < SA::PASSES) la.template issue<RAGGED>(oa, p, h, smem + slot, wv, lane);
+        else lb.template issue<RAGGED>(ob, p - SA::PASSES, h, smem + slot, wv, lane);
+    };
+    constexpr int EARLY = TM * TN == 1 ? PASSES : PASSES / 2;   // pieces requested right behind the barrier, the others a step later
+#pragma unroll
+    for (int s = 0; s < NS; ++s)
+#pragma unroll
+        for (int p = 0; p < (s < NS - 1 ? PASSES : EARLY); ++p) issue_piece(p, s, s * STAGE);
+
+    FragReader<T, OA::kAlong, BM, TM> fa;
+    FragReader<T, OB::kAlong, BN, TN> fb;
+    fa.init(wm * TM, lane);
+    fb.init(wn * TN, lane);
+    typename DenseFrag<T>::type a[2][TM], b[2][TN];
+    // fragment f of a step, in the order the products take them: a[0], the b's, the other a's
+    auto read_frag = [&](int f, int slot, int kk, int set) {
+        if (f >= 1 && f <= TN) b[set][f - 1] = fb.read(smem + slot + BM * kLineBytes, f - 1, kk);
+        else a[set][f ? f - TN : 0] = fa.read(smem + slot, f ? f - TN : 0, kk);
+    };
+    __builtin_amdgcn_s_waitcnt(vmcnt_imm((NS - 2) * PASSES + EARLY));
+    __syncthreads();
+#pragma unroll
+    for (int f = 0; f < TM + TN; ++f) read_frag(f, 0, 0, 0);
+    // (opaque: a value that is a load here and in the loop is loaded where it is used, behind everything that was to hide it)
+#pragma unroll
+    for (int i = 0; i < TM; ++i) asm volatile("" : "+v"(a[0][i]));
+#pragma unroll
+    for (int j = 0; j < TN; ++j) asm volatile("" : "+v"(b[0][j]));
+    int slot = 0, before = (NS - 1) * STAGE;   // of stage h and of the one before it
+    for (int h = 0; h < n_st; ++h) {
+        const int after = slot == (NS - 1) * STAGE ? 0 : slot + STAGE;
+#pragma unroll
+        for (int kk = 0; kk < KSTEPS; ++kk) {
+            constexpr int N_MMA = TM * TN, N_FRAG = TM + TN, N_READ = N_MMA > N_FRAG ? N_FRAG : (N_MMA + 1) / 2;
+            const bool last = kk + 1 == KSTEPS;
+            if (last) {
+                __builtin_amdgcn_s_waitcnt(kLgkm0);
+                __builtin_amdgcn_s_waitcnt(vmcnt_imm((NS - 2) * PASSES));
+                asm volatile("" ::: "memory");
+                __builtin_amdgcn_s_barrier();
+                asm volatile("" ::: "memory");
+            }
+#pragma unroll
+            for (int m = 0; m < N_MMA; ++m) {
+#pragma unroll
+                for (int f = m * N_FRAG / N_READ; f < (m + 1) * N_FRAG / N_READ && f < N_FRAG; ++f)
+                    read_frag(f, last ? after : slot, last ? 0 : kk + 1, (kk + 1) & 1);
+                if (N_MMA > 1) dense_mma(acc[m / TN][m % TN], a[kk & 1][m / TN], b[kk & 1][m % TN]);
+                if (last) {
+#pragma unroll
+                    for (int p = m * EARLY / N_MMA; p < (m + 1) * EARLY / N_MMA; ++p) issue_piece(p, h + NS, slot);
+                }
+                if (kk == 0) {
+#pragma unroll
+                    for (int p = EARLY + m * (PASSES - EARLY) / N_MMA; p < EARLY + (m + 1) * (PASSES - EARLY) / N_MMA; ++p) issue_piece(p, h + NS - 1, before);
+                }
+                if (N_MMA == 1) dense_mma(acc[0][0], a[kk & 1][0], b[kk & 1][0]);   // (it waits for the one before: requests first)
+                __builtin_amdgcn_sched_barrier(0);
+            }
+        }
+        before = slot;
+        slot = after;
+    }
+    __builtin_amdgcn_s_waitcnt(vmcnt_imm(0));   // the stages requested again may still be landing in the ring
     __syncthreads();
 }
 
@@ -362,7 +547,8 @@ __global__ __launch_bounds__(256) void k_dense_join(const float* __restrict__ pa
 }
 
 // M x N results (PAIR: of both products) of `stages` stages of K, in `parts` parts that are summed from `part` by a second launch.
-template <typename T, int BM, int BN, int WGM, int WGN, bool PAIR, class OA, class OB, class Out>
+// NS: stages of the ring of direct loads, 0: staged through registers.
+template <typename T, int BM, int BN, int WGM, int WGN, int NS, bool RAGGED, bool PAIR, class OA, class OB, class Out>
 __global__ __launch_bounds__(WGM * WGN * 64) void k_dense(OA oa, OB ob, int M, int N, int stages, int parts, Out out, float* part) {
     extern __shared__ __attribute__((aligned(1024))) unsigned char smem[];
     constexpr int COLS = PAIR ? BN / 2 : BN, V = kPiece<T>;
@@ -371,9 +557,10 @@ __global__ __launch_bounds__(WGM * WGN * 64) void k_dense(OA oa, OB ob, int M, i
     const int m0 = tile_m * BM, n0 = tile_n * COLS;
     oa.move(m0);
     ob.move(n0);
-    const int h0 = (int)((long long)blockIdx.y * stages / parts), h1 = (int)((long long)(blockIdx.y + 1) * stages / parts);
+    const int h0 = parts == 1 ? 0 : (int)((long long)blockIdx.y * stages / parts), h1 = parts == 1 ? stages : (int)((long long)(blockIdx.y + 1) * stages / parts);
     f32x16_t acc[BM / WGM / 32][BN / WGN / 32];
-    product_of_tile<T, BM, BN, WGM, WGN>(smem, oa, ob, h0, h1, acc);
+    if constexpr (NS > 0) direct_product_of_tile<T, BM, BN, WGM, WGN, NS, RAGGED>(smem, oa, ob, h0, h1, acc);
+    else product_of_tile<T, BM, BN, WGM, WGN>(smem, oa, ob, h0, h1, acc);
     if (parts > 1) {
         const long long pitch = PAIR ? 2ll * N : N;
         PartOut to{part + (size_t)blockIdx.y * M * pitch, N, pitch};
@@ -385,13 +572,12 @@ __global__ __launch_bounds__(WGM * WGN * 64) void k_dense(OA oa, OB ob, int M, i
     else tile_as_rows<BM, BN, WGM, WGN, V>(smem, acc, m0, n0, M, N, out);
 }
 
-template <typename T, int BM, int BN, int WGM, int WGN, bool PAIR, class OA, class OB, class Out>
-static srigl_status launch_dense(const OA& oa, const OB& ob, int M, int N, int stages, int parts, const Out& out, float* part, hipStream_t st) {
-    constexpr size_t ring = (size_t)(BM + BN) * kLineBytes, rows = rows_lds<BM, BN, WGM>(), lds = ring > rows ? ring : rows;
+template <typename T, int BM, int BN, int WGM, int WGN, int NS, bool RAGGED, bool PAIR, class OA, class OB, class Out>
+static srigl_status launch_tiles(const OA& oa, const OB& ob, int M, int N, int stages, int parts, const Out& out, float* part, hipStream_t st) {
+    constexpr size_t ring = (size_t)std::max(NS, 1) * (BM + BN) * kLineBytes, rows = rows_lds<BM, BN, WGM>(), lds = ring > rows ? ring : rows;
     static_assert(lds <= kLdsMax, "LDS");
-    if (M <= 0 || N <= 0) return SRIGL_OK;
     constexpr int COLS = PAIR ? BN / 2 : BN;
-    auto kern = k_dense<T, BM, BN, WGM, WGN, PAIR, OA, OB, Out>;
+    auto kern = k_dense<T, BM, BN, WGM, WGN, NS, RAGGED, PAIR, OA, OB, Out>;
     static LdsLimit limit;
     if (limit.ensure(kern, lds) != SRIGL_OK) return SRIGL_ERR_HIP;
     const long long tiles = ((M + BM - 1ll) / BM) * ((N + COLS - 1ll) / COLS), n_wg = (tiles + kXcds - 1) / kXcds * kXcds;
@@ -402,6 +588,30 @@ static srigl_status launch_dense(const OA& oa, const OB& ob, int M, int N, int s
         hipLaunchKernelGGL((k_dense_join<Out, 4, PAIR>), grid, dim3(256), 0, st, part, parts, M, N, out);
     }
     return hip_ok(hipGetLastError());
+}
+
+// Tile and parts of K of a product (of a pair: N neurons, two sums each)
+struct DensePlan { int tile, parts; };
+enum { kTileS = 0, kTileM = 1, kTileL = 2 };   // 64 x 64 (of a pair 64 x 128), 128 x 128, 256 x 256 (bf16)
+DensePlan plan_dense(int M, int N, int stages, bool f32, bool pair, bool may_split);
+
+template <typename T, bool PAIR, class OA, class OB, class Out>
+static srigl_status launch_dense(const OA& oa, const OB& ob, int M, int N, int stages, DensePlan plan, const Out& out, float* part, hipStream_t st) {
+    if (M <= 0 || N <= 0) return SRIGL_OK;
+    constexpr int SN = PAIR ? 128 : 64;
+    const bool direct = oa.direct(256) && ob.direct(256), ragged = oa.ragged() || ob.ragged();
+    if (!direct) {
+        if (plan.tile == kTileS) return launch_tiles<T, 64, SN, 2, 2, 0, true, PAIR>(oa, ob, M, N, stages, plan.parts, out, part, st);
+        return launch_tiles<T, 128, 128, 2, 2, 0, true, PAIR>(oa, ob, M, N, stages, plan.parts, out, part, st);
+    }
+#define SRIGL_DIRECT(...) \
+    return ragged ? launch_tiles<T, __VA_ARGS__, true, PAIR>(oa, ob, M, N, stages, plan.parts, out, part, st) \
+                  : launch_tiles<T, __VA_ARGS__, false, PAIR>(oa, ob, M, N, stages, plan.parts, out, part, st)
+    if constexpr (sizeof(T) == 2)
+        if (plan.tile == kTileL) SRIGL_DIRECT(256, 256, 2, 4, 2);
+    if (plan.tile != kTileS) SRIGL_DIRECT(128, 128, 2, 2, 4);
+    SRIGL_DIRECT(64, SN, 2, 2, 4);
+#undef SRIGL_DIRECT
 }
 template <typename T> inline int stages_of(long long K) { return (int)((K + kStageK<T> - 1) / kStageK<T>); }
 

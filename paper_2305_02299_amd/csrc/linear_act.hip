@@ -8,6 +8,26 @@
 
 namespace srigl {
 
+// Expected time (us) of a product in a tile: rounds of workgroups over the compute units, each a fixed part and a part per 1000 elements of K.
+struct DenseModel { int bm, bn; float fixed, round, per_k; int slots; };
+static const DenseModel kDenseBf16[] = {{64, 64, 2.8f, 1.1f, 5.6f, 512}, {128, 128, 3.1f, 3.0f, 7.0f, 256}, {256, 256, 0.7f, 7.0f, 20.2f, 256}};
+static const DenseModel kDenseF32[] = {{64, 64, 2.1f, 1.0f, 38.0f, 512}, {128, 128, 2.1f, 2.0f, 70.0f, 256}};
+static const DenseModel kPairBf16 = {64, 128, 2.0f, 3.0f, 5.0f, 256}, kPairF32 = {64, 128, 2.1f, 2.0f, 38.0f, 256};
+
+DensePlan plan_dense(int M, int N, int stages, bool f32, bool pair, bool may_split) {
+    DensePlan best{kTileS, 1};
+    double best_us = 0.0;
+    const double d = 1e-3 * stages * (f32 ? 32 : 64);
+    for (int t = 0; t < (f32 ? 2 : 3); ++t) {
+        const DenseModel& m = pair && t == kTileS ? (f32 ? kPairF32 : kPairBf16) : (f32 ? kDenseF32 : kDenseBf16)[t];
+        const long long cols = pair ? m.bn / 2 : m.bn, tiles = ((M + m.bm - 1ll) / m.bm) * ((N + cols - 1) / cols);
+        const double crowd = m.slots == 512 && tiles <= 256 ? 0.65 : 1.0;   // (alone on its compute unit)
+        const double us = m.fixed + std::ceil((double)tiles / m.slots) * (m.round + crowd * m.per_k * d);
+        if (t == 0 || us < best_us) best = {t, 1}, best_us = us;
+    }
+    return best;
+}
+
 template <typename T, typename TY>
 struct LinearOut {
     const int32_t* active;
@@ -124,16 +144,16 @@ static srigl_status linear_act(const void* x, int B, int d_in, const void* Wd, c
     }
     const RowsOf<T> a{(const T*)x, d_in, B - 1, d_in}, w{(const T*)Wd, d_in, n - 1, d_in};
     const LinearOut<T, TY> out{n == d_out ? nullptr : active, n, bias, (const TY*)residual, d_out, (TY*)y, (T*)z, act, {}};
-    return launch_dense<T, 64, 64, 2, 2, false>(a, w, B, n, stages_of<T>(d_in), 1, out, nullptr, st);
+    return launch_dense<T, false>(a, w, B, n, stages_of<T>(d_in), plan_dense(B, n, stages_of<T>(d_in), sizeof(T) == 4, false, false), out, nullptr, st);
 }
 
 template <typename T>
 static srigl_status gated(const void* x, int B, int d_in, const void* Wg, const void* Wu, int n, const float* bias_g, const float* bias_u, int act, void* h, void* g,
                           void* u, hipStream_t st) {
     const RowsOf<T> a{(const T*)x, d_in, B - 1, d_in};
-    const PairedRows<T, 32> w{(const T*)Wg, (const T*)Wu, d_in, n - 1, d_in};
+    const PairedRows<T, 32> w{(const T*)Wg, bytes_between(Wg, Wu), d_in, n - 1, d_in};
     const GatedOut<T> out{bias_g, bias_u, n, (T*)h, (T*)g, (T*)u, act, {}, {}};
-    return launch_dense<T, 64, 128, 2, 2, true>(a, w, B, n, stages_of<T>(d_in), 1, out, nullptr, st);
+    return launch_dense<T, true>(a, w, B, n, stages_of<T>(d_in), plan_dense(B, n, stages_of<T>(d_in), sizeof(T) == 4, true, false), out, nullptr, st);
 }
 
 }  // namespace srigl

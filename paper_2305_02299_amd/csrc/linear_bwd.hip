@@ -153,11 +153,11 @@ static srigl_status linear_bwd(const BwdPlan& p, const void* dy, const void* x, 
     if (rc == SRIGL_OK && dx) {
         const RowsOf<T> a{dz, pitch, B - 1, pitch};
         const ColsOf<T> w{(const T*)Wd, d_in, d_in, n};
-        rc = launch_dense<T, 64, 64, 2, 2, false>(a, w, B, d_in, stages_of<T>(n), 1, PlainOut<T>{(T*)dx, d_in}, nullptr, st);
+        rc = launch_dense<T, false>(a, w, B, d_in, stages_of<T>(n), plan_dense(B, d_in, stages_of<T>(n), sizeof(T) == 4, false, false), PlainOut<T>{(T*)dx, d_in}, nullptr, st);
     }
     if (rc == SRIGL_OK && dWd) {
         const ColsOf<T> a{dz, pitch, pitch, B}, b{(const T*)x, d_in, d_in, B};
-        rc = launch_dense<T, 64, 64, 2, 2, false>(a, b, n, d_in, stages_of<T>(B), 1, PlainOut<T>{(T*)dWd, d_in}, nullptr, st);
+        rc = launch_dense<T, false>(a, b, n, d_in, stages_of<T>(B), plan_dense(n, d_in, stages_of<T>(B), sizeof(T) == 4, false, false), PlainOut<T>{(T*)dWd, d_in}, nullptr, st);
     }
     return rc;
 }
@@ -177,12 +177,12 @@ static srigl_status gated_bwd(const BwdPlan& p, const void* dh, const void* x, i
     srigl_status rc = hip_ok(hipGetLastError());
     if (rc == SRIGL_OK && dx) {
         const RowsOf<T> a{dz, 2ll * pitch, B - 1, 2 * pitch};
-        const PairedCols<T> w{(const T*)Wg, (const T*)Wu, d_in, d_in, n, pitch};
-        rc = launch_dense<T, 64, 64, 2, 2, false>(a, w, B, d_in, stages_of<T>(2ll * pitch), 1, PlainOut<T>{(T*)dx, d_in}, nullptr, st);
+        const PairedCols<T> w{(const T*)Wg, bytes_between(Wg, Wu), d_in, d_in, n, pitch};
+        rc = launch_dense<T, false>(a, w, B, d_in, stages_of<T>(2ll * pitch), plan_dense(B, d_in, stages_of<T>(2ll * pitch), sizeof(T) == 4, false, false), PlainOut<T>{(T*)dx, d_in}, nullptr, st);
     }
     if (rc == SRIGL_OK && (dWg || dWu) && n > 0) {
         const ColsOf<T> a{dz, 2ll * pitch, 2 * pitch, B}, b{(const T*)x, d_in, d_in, B};
-        rc = launch_dense<T, 64, 64, 2, 2, false>(a, b, 2 * pitch, d_in, stages_of<T>(B), 1, TwoOut<T>{(T*)dWg, (T*)dWu, d_in, n, pitch}, nullptr, st);
+        rc = launch_dense<T, false>(a, b, 2 * pitch, d_in, stages_of<T>(B), plan_dense(2 * pitch, d_in, stages_of<T>(B), sizeof(T) == 4, false, false), TwoOut<T>{(T*)dWg, (T*)dWu, d_in, n, pitch}, nullptr, st);
     }
     return rc;
 }

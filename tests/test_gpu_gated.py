@@ -10,6 +10,7 @@ pytestmark = pytest.mark.gpu
 
 SIZES = [(1, 1, 1), (1, 8, 3), (2, 64, 64), (3, 65, 66), (1, 768, 1000), (4, 4096, 130), (7, 300, 513), (16, 72, 257), (37, 1001, 777), (64, 128, 128), (65, 136, 129),
          (130, 520, 260), (200, 33, 40), (257, 264, 390), (300, 1024, 520)]
+LARGE = [(1500, 264, 4500), (1100, 8200, 264), (200, 4104, 3000), (2048, 256, 4096), (1024, 8192, 256)]
 
 
 def _block(gen, d_in, n, t, make, biased, act):
@@ -21,7 +22,7 @@ def _block(gen, d_in, n, t, make, biased, act):
 
 @pytest.mark.parametrize("biased", [False, True])
 @pytest.mark.parametrize("dtype", ["f32", "bf16"])
-@pytest.mark.parametrize("size", SIZES)
+@pytest.mark.parametrize("size", SIZES + LARGE)
 def test_whole_numbers_come_out_exactly(size, dtype, biased):
     B, d_in, n = size
     gen, t = torch.Generator().manual_seed(B + 7 * d_in + 31 * n), TYPES[dtype]

@@ -11,6 +11,8 @@ pytestmark = pytest.mark.gpu
 # (batch, d_in, d_out): one of everything, whole tiles, a little more and less than tiles and stages, rows that begin anywhere, long sums, few and many rows
 SIZES = [(1, 1, 1), (1, 8, 3), (2, 64, 64), (3, 65, 66), (1, 768, 1000), (4, 4096, 130), (7, 300, 513), (16, 72, 257), (37, 1001, 777), (64, 128, 128), (65, 136, 129),
          (130, 520, 260), (200, 33, 40), (257, 264, 390), (300, 1024, 520), (33, 2056, 96)]
+# (large enough for the largest tiles in one of the three products each, whole stages of K and not)
+LARGE = [(1500, 264, 9000), (1100, 8200, 264), (200, 4104, 5000), (2048, 256, 8192), (1024, 8192, 256)]
 
 
 def _layer(gen, d_in, d_out, ablated, t, make, biased=True):
@@ -25,7 +27,7 @@ def _cuda(*ts):
 
 @pytest.mark.parametrize("ablated", [0.0, 0.3, 0.97])
 @pytest.mark.parametrize("dtype", ["f32", "bf16"])
-@pytest.mark.parametrize("size", SIZES)
+@pytest.mark.parametrize("size", SIZES + LARGE)
 def test_whole_numbers_come_out_exactly(size, dtype, ablated):
     """Sums of small whole numbers are exact in fp32 in any order: every bit of the result and of the gradients is known."""
     B, d_in, d_out = size
