@@ -46,7 +46,8 @@ template <typename T, int V> struct AnyPlace { typedef T type __attribute__((ext
 // ---- operands ----
 // line(l, first, valid): where elements first .. of line l begin, *valid how many of them there are (<= 0: none).
 // For loads that go straight into the LDS, of operands whose lines begin at and are multiples of 16 bytes: stage(h, l) is the scalar address that lane_offset(l, first) bytes are
-// added to (l: any line of the 1 KB that the wavefront's load fills, whose lines are of one matrix), with lines and columns past the last one at the last one; past(h, l, first): behind the end of K.
+// added to (l: any line of the 1 KB that the wavefront's load fills, whose lines are of one matrix), with lines and columns past the last one at the last one.
+// Stages by number: whole() of them have all of their K, the i-th of these being stage index(i); of tails() others, stage tail(t), a part lies behind the end of K.
 // Along K: line = tile row, elements = k.
 template <typename T> struct RowsOf {
     static constexpr bool kAlong = true;
@@ -57,9 +58,11 @@ template <typename T> struct RowsOf {
     __device__ const T* line(int l, int first, int* valid) const { *valid = K - first; return base + (size_t)min(l, last) * pitch + first; }
     __device__ const unsigned char* stage(int h, int) const { return reinterpret_cast<const unsigned char*>(base) + (size_t)h * kLineBytes; }
     __device__ uint32_t lane_offset(int l, int first) const { return ((uint32_t)min(l, last) * (uint32_t)pitch + first) * (uint32_t)sizeof(T); }
-    __device__ bool past(int h, int, int first) const { return h * kStageK<T> + first >= K; }
     bool direct(int lines) const { return direct_rows(base, pitch, lines) && K % kPiece<T> == 0; }
-    bool ragged() const { return K % kStageK<T> != 0; }
+    __device__ int whole() const { return K / kStageK<T>; }
+    __device__ int index(int i) const { return i; }
+    __device__ int tails() const { return K % kStageK<T> ? 1 : 0; }
+    __device__ int tail(int) const { return K / kStageK<T>; }
 };
 // The weight rows of two matrices that a gated block multiplies with, next to each other in each wavefront's part of the tile: HALF rows of the first,
 // the same HALF rows of the second.
@@ -80,9 +83,11 @@ template <typename T, int HALF> struct PairedRows {
     __device__ uint32_t lane_offset(int l, int first) const {
         return ((uint32_t)min((l / HALF >> 1) * HALF + l % HALF, last) * (uint32_t)pitch + first) * (uint32_t)sizeof(T);
     }
-    __device__ bool past(int h, int, int first) const { return h * kStageK<T> + first >= K; }
     bool direct(int lines) const { return direct_rows(base, pitch, lines) && to_second % 16 == 0 && K % kPiece<T> == 0; }
-    bool ragged() const { return K % kStageK<T> != 0; }
+    __device__ int whole() const { return K / kStageK<T>; }
+    __device__ int index(int i) const { return i; }
+    __device__ int tails() const { return K % kStageK<T> ? 1 : 0; }
+    __device__ int tail(int) const { return K / kStageK<T>; }
 };
 // Across K: line = k, elements = tile columns.
 template <typename T> struct ColsOf {
@@ -94,9 +99,11 @@ template <typename T> struct ColsOf {
     __device__ const T* line(int l, int first, int* valid) const { *valid = l < K ? cols - first : 0; return base + (size_t)l * pitch + first; }
     __device__ const unsigned char* stage(int h, int) const { return reinterpret_cast<const unsigned char*>(base + (size_t)h * kStageK<T> * pitch); }
     __device__ uint32_t lane_offset(int l, int first) const { return ((uint32_t)l * (uint32_t)pitch + min(first, cols - kPiece<T>)) * (uint32_t)sizeof(T); }
-    __device__ bool past(int h, int l, int) const { return h * kStageK<T> + l >= K; }
     bool direct(int) const { return direct_rows(base, pitch, kStageK<T>) && cols % kPiece<T> == 0; }
-    bool ragged() const { return K % kStageK<T> != 0; }
+    __device__ int whole() const { return K / kStageK<T>; }
+    __device__ int index(int i) const { return i; }
+    __device__ int tails() const { return K % kStageK<T> ? 1 : 0; }
+    __device__ int tail(int) const { return K / kStageK<T>; }
 };
 // Lines 0 .. n - 1 of one matrix, then, from line `padded` on, those of a second.
 template <typename T> struct PairedCols {
@@ -118,12 +125,12 @@ template <typename T> struct PairedCols {
         return reinterpret_cast<const unsigned char*>(of(h >= in_first) + (size_t)(h >= in_first ? h - in_first : h) * kStageK<T> * pitch);
     }
     __device__ uint32_t lane_offset(int l, int first) const { return ((uint32_t)l * (uint32_t)pitch + min(first, cols - kPiece<T>)) * (uint32_t)sizeof(T); }
-    __device__ bool past(int h, int l, int) const {
-        const int k = h * kStageK<T> + l;
-        return (k >= padded ? k - padded : k) >= n;
-    }
+    // (in_first * kStageK may reach a whole stage behind n: that one is left out)
+    __device__ int whole() const { return 2 * (n / kStageK<T>); }
+    __device__ int index(int i) const { const int w = n / kStageK<T>; return i < w ? i : i - w + padded / kStageK<T>; }
+    __device__ int tails() const { return n % kStageK<T> ? 2 : 0; }
+    __device__ int tail(int t) const { return n / kStageK<T> + t * (padded / kStageK<T>); }
     bool direct(int) const { return direct_rows(base, pitch, kStageK<T>) && to_second % 16 == 0 && cols % kPiece<T> == 0; }
-    bool ragged() const { return n != padded; }
 };
 
 // 16 bytes from there, zeros behind the valid elements
@@ -223,18 +230,12 @@ struct RegStage {
     }
 };
 
+// Stages h0 .. h1 - 1, whatever part of them there is
 template <typename T, int BM, int BN, int WGM, int WGN, class OA, class OB>
-__device__ __forceinline__ void product_of_tile(unsigned char* smem, const OA& oa, const OB& ob, int h0, int h1,
-                                                f32x16_t (&acc)[BM / WGM / 32][BN / WGN / 32]) {
+__device__ __forceinline__ void product_of_tile(unsigned char* smem, const OA& oa, const OB& ob, int h0, int h1, f32x16_t (&acc)[BM / WGM / 32][BN / WGN / 32]) {
     constexpr int NT = WGM * WGN * 64, TM = BM / WGM / 32, TN = BN / WGN / 32, KSTEPS = kLineBytes / 32;
     const int lane = threadIdx.x & 63, wv = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), wm = wv / WGN, wn = wv % WGN;
     unsigned char *const sa = smem, *const sb = smem + BM * kLineBytes;
-#pragma unroll
-    for (int i = 0; i < TM; ++i)
-#pragma unroll
-        for (int j = 0; j < TN; ++j)
-#pragma unroll
-            for (int e = 0; e < 16; ++e) acc[i][j][e] = 0.0f;
     if (h0 >= h1) return;
     FragReader<T, OA::kAlong, BM, TM> fa;
     FragReader<T, OB::kAlong, BN, TN> fb;
@@ -292,21 +293,16 @@ struct DirectStage {
             at[p] = op.lane_offset(l, first);
         }
     }
-    template <bool RAGGED>
-    __device__ __forceinline__ void issue(const Op& op, int p, int h, unsigned char* stage, int wv, int lane) const {
+    __device__ __forceinline__ void issue(const Op& op, int p, int h, unsigned char* stage, int wv) const {
         uint32_t off = at[p];
         asm("" : "+v"(off));   // (a lane offset from a scalar base: seen to be 32 bits only next to the load)
         const unsigned char* g = op.stage(h, (p * NWAVES + wv) * 64 / PER_LINE) + off;
-        if (RAGGED) {
-            int l, first;
-            place(p, wv, lane, &l, &first);
-            if (op.past(h, l, first)) g = reinterpret_cast<const unsigned char*>(&g_zero16);
-        }
         __builtin_amdgcn_global_load_lds((gptr_t)g, (lptr_t)(stage + FIRST + 1024 * (p * NWAVES + wv)), 16, 0, 0);
     }
 };
 
-template <typename T, int BM, int BN, int WGM, int WGN, int NS, bool RAGGED, class OA, class OB>
+// Whole stages h0 .. h1 - 1, by their number.  (The part of a stage behind the end of K in the loop, its pieces from zeros by lane: 20 % longer in 128 x 128 tiles.)
+template <typename T, int BM, int BN, int WGM, int WGN, int NS, class OA, class OB>
 __device__ __forceinline__ void direct_product_of_tile(unsigned char* smem, const OA& oa, const OB& ob, int h0, int h1, f32x16_t (&acc)[BM / WGM / 32][BN / WGN / 32]) {
     constexpr int NWAVES = WGM * WGN, TM = BM / WGM / 32, TN = BN / WGN / 32, KSTEPS = kLineBytes / 32, STAGE = (BM + BN) * kLineBytes;
     using SA = DirectStage<T, BM, 0, NWAVES, OA>;
@@ -314,21 +310,15 @@ __device__ __forceinline__ void direct_product_of_tile(unsigned char* smem, cons
     constexpr int PASSES = SA::PASSES + SB::PASSES;
     static_assert(NS >= 2 && (NS - 1) * PASSES <= 63, "vmcnt range");
     const int lane = threadIdx.x & 63, wv = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), wm = wv / WGN, wn = wv % WGN, n_st = h1 - h0;
-#pragma unroll
-    for (int i = 0; i < TM; ++i)
-#pragma unroll
-        for (int j = 0; j < TN; ++j)
-#pragma unroll
-            for (int e = 0; e < 16; ++e) acc[i][j][e] = 0.0f;
     if (n_st <= 0) return;
     SA la;
     SB lb;
     la.init(oa, wv, lane);
     lb.init(ob, wv, lane);
     auto issue_piece = [&](int p, int h_unclamped, int slot) {
-        const int h = h0 + min(h_unclamped, n_st - 1);
-        if (p < SA::PASSES) la.template issue<RAGGED>(oa, p, h, smem + slot, wv, lane);
-        else lb.template issue<RAGGED>(ob, p - SA::PASSES, h, smem + slot, wv, lane);
+        const int h = ob.index(h0 + min(h_unclamped, n_st - 1));
+        if (p < SA::PASSES) la.issue(oa, p, h, smem + slot, wv);
+        else lb.issue(ob, p - SA::PASSES, h, smem + slot, wv);
     };
     constexpr int EARLY = TM * TN == 1 ? PASSES : PASSES / 2;   // pieces requested right behind the barrier, the others a step later
 #pragma unroll
@@ -529,6 +519,7 @@ __global__ __launch_bounds__(256) void k_dense_join(const float* __restrict__ pa
     const long long pitch = PAIR ? 2ll * N : N;
     for (int m = blockIdx.y; m < M; m += gridDim.y) {
         float v[V] = {}, w[V] = {};
+#pragma unroll 4
         for (int z = 0; z < parts; ++z) {
             const float* const p = part + ((size_t)z * M + m) * pitch + c;
             float t[V];
@@ -548,7 +539,7 @@ __global__ __launch_bounds__(256) void k_dense_join(const float* __restrict__ pa
 
 // M x N results (PAIR: of both products) of `stages` stages of K, in `parts` parts that are summed from `part` by a second launch.
 // NS: stages of the ring of direct loads, 0: staged through registers.
-template <typename T, int BM, int BN, int WGM, int WGN, int NS, bool RAGGED, bool PAIR, class OA, class OB, class Out>
+template <typename T, int BM, int BN, int WGM, int WGN, int NS, bool PAIR, class OA, class OB, class Out>
 __global__ __launch_bounds__(WGM * WGN * 64) void k_dense(OA oa, OB ob, int M, int N, int stages, int parts, Out out, float* part) {
     extern __shared__ __attribute__((aligned(1024))) unsigned char smem[];
     constexpr int COLS = PAIR ? BN / 2 : BN, V = kPiece<T>;
@@ -557,10 +548,22 @@ __global__ __launch_bounds__(WGM * WGN * 64) void k_dense(OA oa, OB ob, int M, i
     const int m0 = tile_m * BM, n0 = tile_n * COLS;
     oa.move(m0);
     ob.move(n0);
+    if (NS > 0) stages = ob.whole();
     const int h0 = parts == 1 ? 0 : (int)((long long)blockIdx.y * stages / parts), h1 = parts == 1 ? stages : (int)((long long)(blockIdx.y + 1) * stages / parts);
     f32x16_t acc[BM / WGM / 32][BN / WGN / 32];
-    if constexpr (NS > 0) direct_product_of_tile<T, BM, BN, WGM, WGN, NS, RAGGED>(smem, oa, ob, h0, h1, acc);
-    else product_of_tile<T, BM, BN, WGM, WGN>(smem, oa, ob, h0, h1, acc);
+#pragma unroll
+    for (int i = 0; i < BM / WGM / 32; ++i)
+#pragma unroll
+        for (int j = 0; j < BN / WGN / 32; ++j)
+#pragma unroll
+            for (int e = 0; e < 16; ++e) acc[i][j][e] = 0.0f;
+    if constexpr (NS > 0) {
+        direct_product_of_tile<T, BM, BN, WGM, WGN, NS>(smem, oa, ob, h0, h1, acc);
+        if ((int)blockIdx.y == parts - 1)
+            for (int t = 0; t < ob.tails(); ++t) product_of_tile<T, BM, BN, WGM, WGN>(smem, oa, ob, ob.tail(t), ob.tail(t) + 1, acc);
+    } else {
+        product_of_tile<T, BM, BN, WGM, WGN>(smem, oa, ob, h0, h1, acc);
+    }
     if (parts > 1) {
         const long long pitch = PAIR ? 2ll * N : N;
         PartOut to{part + (size_t)blockIdx.y * M * pitch, N, pitch};
@@ -572,12 +575,12 @@ __global__ __launch_bounds__(WGM * WGN * 64) void k_dense(OA oa, OB ob, int M, i
     else tile_as_rows<BM, BN, WGM, WGN, V>(smem, acc, m0, n0, M, N, out);
 }
 
-template <typename T, int BM, int BN, int WGM, int WGN, int NS, bool RAGGED, bool PAIR, class OA, class OB, class Out>
+template <typename T, int BM, int BN, int WGM, int WGN, int NS, bool PAIR, class OA, class OB, class Out>
 static srigl_status launch_tiles(const OA& oa, const OB& ob, int M, int N, int stages, int parts, const Out& out, float* part, hipStream_t st) {
     constexpr size_t ring = (size_t)std::max(NS, 1) * (BM + BN) * kLineBytes, rows = rows_lds<BM, BN, WGM>(), lds = ring > rows ? ring : rows;
     static_assert(lds <= kLdsMax, "LDS");
     constexpr int COLS = PAIR ? BN / 2 : BN;
-    auto kern = k_dense<T, BM, BN, WGM, WGN, NS, RAGGED, PAIR, OA, OB, Out>;
+    auto kern = k_dense<T, BM, BN, WGM, WGN, NS, PAIR, OA, OB, Out>;
     static LdsLimit limit;
     if (limit.ensure(kern, lds) != SRIGL_OK) return SRIGL_ERR_HIP;
     const long long tiles = ((M + BM - 1ll) / BM) * ((N + COLS - 1ll) / COLS), n_wg = (tiles + kXcds - 1) / kXcds * kXcds;
@@ -592,26 +595,25 @@ static srigl_status launch_tiles(const OA& oa, const OB& ob, int M, int N, int s
 
 // Tile and parts of K of a product (of a pair: N neurons, two sums each)
 struct DensePlan { int tile, parts; };
-enum { kTileS = 0, kTileM = 1, kTileL = 2 };   // 64 x 64 (of a pair 64 x 128), 128 x 128, 256 x 256 (bf16)
-DensePlan plan_dense(int M, int N, int stages, bool f32, bool pair, bool may_split);
+enum { kTileS = 0, kTileM = 1, kTileH = 2, kTileL = 3 };   // 64 x 64 (of a pair 64 x 128), 128 x 128, 256 x 128 and 256 x 256 (bf16, direct loads)
+DensePlan plan_dense(int M, int N, int stages, bool f32, bool pair, bool direct);
+// bytes of the parts' sums
+inline size_t part_bytes(DensePlan p, int M, int N, bool pair) { return p.parts > 1 ? (size_t)p.parts * M * N * (pair ? 2 : 1) * sizeof(float) : 0; }
 
 template <typename T, bool PAIR, class OA, class OB, class Out>
 static srigl_status launch_dense(const OA& oa, const OB& ob, int M, int N, int stages, DensePlan plan, const Out& out, float* part, hipStream_t st) {
     if (M <= 0 || N <= 0) return SRIGL_OK;
     constexpr int SN = PAIR ? 128 : 64;
-    const bool direct = oa.direct(256) && ob.direct(256), ragged = oa.ragged() || ob.ragged();
-    if (!direct) {
-        if (plan.tile == kTileS) return launch_tiles<T, 64, SN, 2, 2, 0, true, PAIR>(oa, ob, M, N, stages, plan.parts, out, part, st);
-        return launch_tiles<T, 128, 128, 2, 2, 0, true, PAIR>(oa, ob, M, N, stages, plan.parts, out, part, st);
+    if (!(oa.direct(256) && ob.direct(256))) {
+        if (plan.tile == kTileS) return launch_tiles<T, 64, SN, 2, 2, 0, PAIR>(oa, ob, M, N, stages, plan.parts, out, part, st);
+        return launch_tiles<T, 128, 128, 2, 2, 0, PAIR>(oa, ob, M, N, stages, plan.parts, out, part, st);
     }
-#define SRIGL_DIRECT(...) \
-    return ragged ? launch_tiles<T, __VA_ARGS__, true, PAIR>(oa, ob, M, N, stages, plan.parts, out, part, st) \
-                  : launch_tiles<T, __VA_ARGS__, false, PAIR>(oa, ob, M, N, stages, plan.parts, out, part, st)
-    if constexpr (sizeof(T) == 2)
-        if (plan.tile == kTileL) SRIGL_DIRECT(256, 256, 2, 4, 2);
-    if (plan.tile != kTileS) SRIGL_DIRECT(128, 128, 2, 2, 4);
-    SRIGL_DIRECT(64, SN, 2, 2, 4);
-#undef SRIGL_DIRECT
+    if constexpr (sizeof(T) == 2) {
+        if (plan.tile == kTileL) return launch_tiles<T, 256, 256, 2, 4, 2, PAIR>(oa, ob, M, N, stages, plan.parts, out, part, st);
+        if (plan.tile == kTileH) return launch_tiles<T, 256, 128, 4, 2, 3, PAIR>(oa, ob, M, N, stages, plan.parts, out, part, st);
+    }
+    if (plan.tile != kTileS) return launch_tiles<T, 128, 128, 2, 2, 4, PAIR>(oa, ob, M, N, stages, plan.parts, out, part, st);
+    return launch_tiles<T, 64, SN, 2, 2, 4, PAIR>(oa, ob, M, N, stages, plan.parts, out, part, st);
 }
 template <typename T> inline int stages_of(long long K) { return (int)((K + kStageK<T> - 1) / kStageK<T>); }
 
@@ -619,6 +621,7 @@ constexpr int kMaxSide = 1 << 30;   // rows and columns of a product
 inline bool known_dtype(srigl_dtype t) { return t == SRIGL_F32 || t == SRIGL_BF16; }
 inline bool known_act(srigl_activation a) { return a == SRIGL_ACT_NONE || a == SRIGL_ACT_RELU || a == SRIGL_ACT_GELU || a == SRIGL_ACT_SILU; }
 inline size_t dtype_bytes(srigl_dtype t) { return t == SRIGL_F32 ? 4 : 2; }
+inline bool scratch_fits(const void* ws, size_t bytes, size_t need) { return need == 0 || (ws != nullptr && bytes >= need); }
 // whether some of the pointers do not stand at an element
 inline bool astray(size_t elem, std::initializer_list<const void*> ps) {
     uintptr_t bits = 0;

@@ -118,12 +118,15 @@ struct TwoOut {
 // What a backward pass takes of the workspace
 struct BwdPlan {
     int chunk_rows, chunks;
-    size_t dz_bytes, sum_bytes, bytes;
+    DensePlan dx, dW;
+    size_t dz_bytes, sum_bytes, bytes;   // the products' parts lie behind both
 };
 static size_t whole(size_t bytes) { return (bytes + 255) / 256 * 256; }
-// cols: columns of dz in a row, padding included; sum_cols: of the sums
-static BwdPlan plan_bwd(int B, long long cols, long long sum_cols, size_t elem) {
+// cols: columns of dz in a row, padding included; K: what dx's product sums over; dW_rows: rows of the weight gradients' product; sum_cols: columns of the sums
+static BwdPlan plan_bwd(int B, int d_in, long long cols, long long K, long long dW_rows, long long sum_cols, size_t elem) {
     BwdPlan p{};
+    const bool f32 = elem == 4, direct = d_in % (16 / (int)elem) == 0;
+
     // about a thousand workgroups of 256 columns, 8 rows to a thread at least
     const long long groups = std::max(1ll, (sum_cols + 255) / 256), want = std::max(1ll, 1024 / groups);
     long long rows = std::max<long long>(8, (B + want - 1) / want);
@@ -132,7 +135,10 @@ static BwdPlan plan_bwd(int B, long long cols, long long sum_cols, size_t elem) 
     p.chunks = (int)((B + (long long)p.chunk_rows - 1) / p.chunk_rows);
     p.dz_bytes = whole((size_t)B * cols * elem);
     p.sum_bytes = whole((size_t)p.chunks * sum_cols * sizeof(float));
-    p.bytes = p.dz_bytes + p.sum_bytes;
+    const auto stages = [&](long long K) { return f32 ? stages_of<float>(K) : stages_of<uint16_t>(K); };
+    p.dx = plan_dense(B, d_in, stages(K), f32, false, direct);
+    p.dW = plan_dense((int)dW_rows, d_in, stages(B), f32, false, direct);
+    p.bytes = p.dz_bytes + p.sum_bytes + whole(std::max(part_bytes(p.dx, B, d_in, false), part_bytes(p.dW, (int)dW_rows, d_in, false)));
     return p;
 }
 
@@ -142,7 +148,7 @@ static srigl_status linear_bwd(const BwdPlan& p, const void* dy, const void* x, 
     const int pitch = (int)padded(n);
     const int32_t* const list = n == d_out ? nullptr : active;
     T* const dz = reinterpret_cast<T*>(ws);
-    float* const sums = reinterpret_cast<float*>(ws + p.dz_bytes);
+    float *const sums = reinterpret_cast<float*>(ws + p.dz_bytes), *const part = reinterpret_cast<float*>(ws + p.dz_bytes + p.sum_bytes);
     if (p.chunks > 0 && (n > 0 || dbias)) {
         const dim3 grid((unsigned)((d_out + (long long)pitch - n + 255) / 256), (unsigned)p.chunks);
         hipLaunchKernelGGL((k_dz_linear<T, TY>), grid, dim3(256), 0, st, (const TY*)dy, (const T*)z, list, n, B, d_out, act, n > 0 ? dz : nullptr, pitch,
@@ -153,11 +159,11 @@ static srigl_status linear_bwd(const BwdPlan& p, const void* dy, const void* x, 
     if (rc == SRIGL_OK && dx) {
         const RowsOf<T> a{dz, pitch, B - 1, pitch};
         const ColsOf<T> w{(const T*)Wd, d_in, d_in, n};
-        rc = launch_dense<T, false>(a, w, B, d_in, stages_of<T>(n), plan_dense(B, d_in, stages_of<T>(n), sizeof(T) == 4, false, false), PlainOut<T>{(T*)dx, d_in}, nullptr, st);
+        rc = launch_dense<T, false>(a, w, B, d_in, stages_of<T>(n), p.dx, PlainOut<T>{(T*)dx, d_in}, part, st);
     }
     if (rc == SRIGL_OK && dWd) {
         const ColsOf<T> a{dz, pitch, pitch, B}, b{(const T*)x, d_in, d_in, B};
-        rc = launch_dense<T, false>(a, b, n, d_in, stages_of<T>(B), plan_dense(n, d_in, stages_of<T>(B), sizeof(T) == 4, false, false), PlainOut<T>{(T*)dWd, d_in}, nullptr, st);
+        rc = launch_dense<T, false>(a, b, n, d_in, stages_of<T>(B), p.dW, PlainOut<T>{(T*)dWd, d_in}, part, st);
     }
     return rc;
 }
@@ -167,7 +173,7 @@ static srigl_status gated_bwd(const BwdPlan& p, const void* dh, const void* x, i
                               int act, void* dx, void* dWg, void* dWu, float* dbias_g, float* dbias_u, unsigned char* ws, hipStream_t st) {
     const int pitch = (int)padded(n);
     T* const dz = reinterpret_cast<T*>(ws);
-    float* const sums = reinterpret_cast<float*>(ws + p.dz_bytes);
+    float *const sums = reinterpret_cast<float*>(ws + p.dz_bytes), *const part = reinterpret_cast<float*>(ws + p.dz_bytes + p.sum_bytes);
     const bool want_sums = dbias_g || dbias_u;
     if (p.chunks > 0 && n > 0)
         hipLaunchKernelGGL(k_dz_gated<T>, dim3((unsigned)((pitch + 255) / 256), (unsigned)p.chunks), dim3(256), 0, st, (const T*)dh, (const T*)g, (const T*)u, n, B, act, dz,
@@ -178,11 +184,11 @@ static srigl_status gated_bwd(const BwdPlan& p, const void* dh, const void* x, i
     if (rc == SRIGL_OK && dx) {
         const RowsOf<T> a{dz, 2ll * pitch, B - 1, 2 * pitch};
         const PairedCols<T> w{(const T*)Wg, bytes_between(Wg, Wu), d_in, d_in, n, pitch};
-        rc = launch_dense<T, false>(a, w, B, d_in, stages_of<T>(2ll * pitch), plan_dense(B, d_in, stages_of<T>(2ll * pitch), sizeof(T) == 4, false, false), PlainOut<T>{(T*)dx, d_in}, nullptr, st);
+        rc = launch_dense<T, false>(a, w, B, d_in, stages_of<T>(2ll * pitch), p.dx, PlainOut<T>{(T*)dx, d_in}, part, st);
     }
     if (rc == SRIGL_OK && (dWg || dWu) && n > 0) {
         const ColsOf<T> a{dz, 2ll * pitch, 2 * pitch, B}, b{(const T*)x, d_in, d_in, B};
-        rc = launch_dense<T, false>(a, b, 2 * pitch, d_in, stages_of<T>(B), plan_dense(2 * pitch, d_in, stages_of<T>(B), sizeof(T) == 4, false, false), TwoOut<T>{(T*)dWg, (T*)dWu, d_in, n, pitch}, nullptr, st);
+        rc = launch_dense<T, false>(a, b, 2 * pitch, d_in, stages_of<T>(B), p.dW, TwoOut<T>{(T*)dWg, (T*)dWu, d_in, n, pitch}, part, st);
     }
     return rc;
 }
@@ -197,7 +203,7 @@ extern "C" {
 
 size_t srigl_structured_bwd_workspace_bytes(int32_t B, int32_t d_in, int32_t n_active, int32_t d_out, srigl_dtype dtype) {
     if (B < 0 || d_in < 0 || n_active < 0 || d_out < n_active || !known_dtype(dtype) || !bwd_sizes_fit(B, d_in, d_out)) return 0;
-    return plan_bwd(B, padded(n_active), d_out, dtype_bytes(dtype)).bytes;
+    return plan_bwd(B, d_in, padded(n_active), n_active, n_active, d_out, dtype_bytes(dtype)).bytes;
 }
 
 srigl_status srigl_structured_linear_bwd(const void* dy, srigl_dtype dy_dtype, const void* x, srigl_dtype x_dtype, int32_t B, int32_t d_in, const void* Wd,
@@ -213,7 +219,7 @@ srigl_status srigl_structured_linear_bwd(const void* dy, srigl_dtype dy_dtype, c
     if (rows && act != SRIGL_ACT_NONE && z == nullptr && (dx || dWd || dbias)) return SRIGL_ERR_INVALID_ARG;
     if (astray(dtype_bytes(x_dtype), {x, Wd, z, dx, dWd}) || astray(dtype_bytes(dy_dtype), {dy}) || astray(4, {bias, active, dbias})) return SRIGL_ERR_INVALID_ARG;
     if (!dx && !dWd && !dbias) return SRIGL_OK;
-    const BwdPlan p = plan_bwd(B, padded(n_active), d_out, dtype_bytes(x_dtype));
+    const BwdPlan p = plan_bwd(B, d_in, padded(n_active), n_active, n_active, d_out, dtype_bytes(x_dtype));
     if (p.bytes > 0 && workspace == nullptr) return SRIGL_ERR_CAPACITY;
     if (workspace_bytes < p.bytes) return SRIGL_ERR_CAPACITY;
     if ((reinterpret_cast<uintptr_t>(workspace) & 15) != 0) return SRIGL_ERR_INVALID_ARG;
@@ -227,7 +233,7 @@ srigl_status srigl_structured_linear_bwd(const void* dy, srigl_dtype dy_dtype, c
 
 size_t srigl_gated_bwd_workspace_bytes(int32_t B, int32_t d_in, int32_t n, srigl_dtype dtype) {
     if (B < 0 || d_in < 0 || n < 0 || !known_dtype(dtype) || !bwd_sizes_fit(B, d_in, n)) return 0;
-    return plan_bwd(B, 2 * padded(n), 2ll * n, dtype_bytes(dtype)).bytes;
+    return plan_bwd(B, d_in, 2 * padded(n), 2 * padded(n), 2 * padded(n), 2ll * n, dtype_bytes(dtype)).bytes;
 }
 
 srigl_status srigl_gated_linear_bwd(const void* dh, const void* x, srigl_dtype x_dtype, int32_t B, int32_t d_in, const void* Wg, const void* Wu, srigl_dtype w_dtype,
@@ -240,7 +246,7 @@ srigl_status srigl_gated_linear_bwd(const void* dh, const void* x, srigl_dtype x
     if (rows && d_in > 0 && ((dx && (Wg == nullptr || Wu == nullptr)) || ((dWg || dWu) && x == nullptr))) return SRIGL_ERR_INVALID_ARG;
     if (astray(dtype_bytes(x_dtype), {dh, x, Wg, Wu, g, u, dx, dWg, dWu}) || astray(4, {dbias_g, dbias_u})) return SRIGL_ERR_INVALID_ARG;
     if (!any) return SRIGL_OK;
-    const BwdPlan p = plan_bwd(B, 2 * padded(n), 2ll * n, dtype_bytes(x_dtype));
+    const BwdPlan p = plan_bwd(B, d_in, 2 * padded(n), 2 * padded(n), 2 * padded(n), 2ll * n, dtype_bytes(x_dtype));
     if (workspace_bytes < p.bytes || (p.bytes > 0 && workspace == nullptr)) return SRIGL_ERR_CAPACITY;
     if ((reinterpret_cast<uintptr_t>(workspace) & 15) != 0) return SRIGL_ERR_INVALID_ARG;
     hipStream_t st = static_cast<hipStream_t>(stream);
