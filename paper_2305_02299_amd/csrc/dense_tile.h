@@ -449,6 +449,88 @@ __device__ __forceinline__ void pair_as_rows(unsigned char* smem, const f32x16_t
     }
 }
 
+// The same where the tile's neurons have places of their own in the result's rows (a list of columns, ablated ones between them): the columns from behind the tile before to this one's
+// last neuron are one range, which passes through the LDS in windows of EL::COLS at its final columns.  out.listed(m, c, first, valid, v, gaps, flat): V columns from c on, of
+// which [first, valid) are this tile's; columns with their bit in gaps are ablated and are `flat`.  out.stored(m, s, valid, v): sums (with bias) of neurons s .. in their own
+// order, where out.wants_stored().
+template <int BM, int BN, int WGM, int WGN, int V, class Out>
+__device__ __forceinline__ void listed_as_rows(unsigned char* smem, const f32x16_t (&acc)[BM / WGM / 32][BN / WGN / 32], int m0, int n0, int M, Out& out) {
+    using EL = EpiLayout<BN, WGM>;
+    constexpr int NT = WGM * WGN * 64, TM = BM / WGM / 32, TN = BN / WGN / 32, PITCH = EL::PITCH, GROUPS = EL::COLS / V, STEP = NT / GROUPS;
+    static_assert(NT % GROUPS == 0 && EL::COLS >= BN, "a thread keeps its columns");
+    float* const tile = reinterpret_cast<float*>(smem);
+    unsigned char* const tables = smem + EL::TILE_BYTES;
+    const int* const place = reinterpret_cast<const int*>(tables);
+    const int* const table = place + BN;
+    float* const tbias = reinterpret_cast<float*>(tables + (size_t)(BN + EL::COLS) * 4);
+    const int tid = threadIdx.x, lane = tid & 63, wv = __builtin_amdgcn_readfirstlane(tid >> 6), wm = wv / WGN, wn = wv % WGN;
+    TileColumns cols = tile_columns(n0, BN, out.active, out.n_active, out.d_out, 0);
+    cols.base = cols.lo / V * V;   // (16-byte stores begin at whole pieces of the row)
+    if (out.wants_stored()) {
+        const int c = (tid % (BN / V)) * V, valid = cols.stored - c;
+        if (valid > 0) out.template start<V>(n0 + c, valid);
+#pragma unroll
+        for (int i = 0; i < TM; ++i) {
+            strip_to_lds<WGN>(tile, PITCH, acc, i);
+            __syncthreads();
+            for (int r = tid / (BN / V); r < 32 * WGM; r += NT / (BN / V)) {
+                const int m = m0 + (r >> 5) * (BM / WGM) + i * 32 + (r & 31);
+                if (m >= M || valid <= 0) continue;
+                float v[V];
+#pragma unroll
+                for (int q = 0; q < V; q += 4) *reinterpret_cast<f32x4_t*>(v + q) = *reinterpret_cast<const f32x4_t*>(tile + r * PITCH + c + q);
+                out.template stored<V>(m, n0 + c, valid, v);
+            }
+            __syncthreads();
+        }
+    }
+    for (int cc = cols.base; cc <= cols.hi; cc += EL::COLS) {
+        const int wc = min(EL::COLS, cols.hi - cc + 1), head = max(cols.lo - cc, 0);
+        if (cc != cols.base) __syncthreads();   // the window before is done with the tables
+        fill_table<BN, WGM, NT>(tables, cc, cols, n0, out.active, out.bias);
+        __syncthreads();
+        int at[TN];   // this lane's columns in the window
+        float add[TN];
+#pragma unroll
+        for (int j = 0; j < TN; ++j) {
+            const int q = place[(wn * TN + j) * 32 + (lane & 31)];
+            at[j] = q < 0 ? -1 : q - (cc - cols.base);
+            if (at[j] >= wc) at[j] = -1;
+            add[j] = tbias[max(at[j], 0)];
+        }
+        const int k0 = (tid % GROUPS) * V, first = max(head - k0, 0), valid = min(V, wc - k0);
+        int gaps = 0;
+        float flat[V];
+#pragma unroll
+        for (int q = 0; q < V; ++q) {
+            const int k = min(max(k0 + q, head), wc - 1);
+            if (table[k] < 0) gaps |= 1 << q;
+            flat[q] = tbias[k];
+        }
+        out.template gap_values<V>(gaps, flat);
+#pragma unroll
+        for (int i = 0; i < TM; ++i) {
+            if (i > 0 || cc != cols.base) __syncthreads();   // the rows before have been read
+#pragma unroll
+            for (int j = 0; j < TN; ++j)
+                if (at[j] >= 0) {
+                    float* const t = tile + (wm * 32 + 4 * (lane >> 5)) * PITCH + at[j];
+#pragma unroll
+                    for (int e = 0; e < 16; ++e) t[(8 * (e >> 2) + (e & 3)) * PITCH] = acc[i][j][e] + add[j];
+                }
+            __syncthreads();
+            for (int r = tid / GROUPS; r < 32 * WGM; r += STEP) {
+                const int m = m0 + (r >> 5) * (BM / WGM) + i * 32 + (r & 31);
+                if (m >= M || valid <= first) continue;
+                float v[V];
+#pragma unroll
+                for (int q = 0; q < V; q += 4) *reinterpret_cast<f32x4_t*>(v + q) = *reinterpret_cast<const f32x4_t*>(tile + r * PITCH + k0 + q);
+                out.template listed<V>(m, cc + k0, first, valid, v, gaps, flat);
+            }
+        }
+    }
+}
+
 // ---- values in and out ----
 __device__ __forceinline__ float to_float(float v) { return v; }
 __device__ __forceinline__ float to_float(uint16_t v) { return bf16_bits_to_float(v); }
@@ -458,8 +540,8 @@ template <typename T> __device__ __forceinline__ T from_float(float v) {
     else return __builtin_bit_cast(uint16_t, (__bf16)v);
 }
 template <typename T, int V>
-__device__ __forceinline__ void store_values(T* p, const float (&v)[V], int valid) {
-    if (valid >= V) {
+__device__ __forceinline__ void store_values(T* p, const float (&v)[V], int valid, int first = 0) {
+    if (valid >= V && first <= 0) {
         typename AnyPlace<T, V>::type w;
 #pragma unroll
         for (int q = 0; q < V; ++q) w[q] = from_float<T>(v[q]);
@@ -467,32 +549,52 @@ __device__ __forceinline__ void store_values(T* p, const float (&v)[V], int vali
     } else {
 #pragma unroll
         for (int q = 0; q < V; ++q)
-            if (q < valid) p[q] = from_float<T>(v[q]);
+            if (q >= first && q < valid) p[q] = from_float<T>(v[q]);
     }
 }
 template <typename T, int V>
-__device__ __forceinline__ void load_values(const T* p, float (&v)[V], int valid) {
-    if (valid >= V) {
+__device__ __forceinline__ void load_values(const T* p, float (&v)[V], int valid, int first = 0) {
+    if (valid >= V && first <= 0) {
         const typename AnyPlace<T, V>::type w = *reinterpret_cast<const typename AnyPlace<T, V>::type*>(p);
 #pragma unroll
         for (int q = 0; q < V; ++q) v[q] = to_float((T)w[q]);
     } else {
 #pragma unroll
-        for (int q = 0; q < V; ++q) v[q] = q < valid ? to_float(p[q]) : 0.0f;
+        for (int q = 0; q < V; ++q) v[q] = q >= first && q < valid ? to_float(p[q]) : 0.0f;
     }
 }
 
-// The activations of these products: apply_act's, and v * sigmoid(v); and their slopes.
+// The activations of these products and their slopes, for millions of values behind a product: one hardware exponential (of two) and one reciprocal each.
+// GELU: Phi(-|v|) = erfc(|v| / sqrt 2) / 2 by Abramowitz and Stegun 7.1.26, a polynomial of degree 5 in t = 1 / (1 + p |v| / sqrt 2) times exp(-v^2 / 2), which is the density's exponential
+// too; |error of erf| <= 1.5e-7, a step or two of fp32 beside 1.  (With erff the epilogue of 2048 x 13108 values was 40 us of vector instructions.)
+// SiLU: the exponential is off by |v| 2^-24 of itself, the reciprocal by a step.  NaN stays NaN in all of them.
+__device__ __forceinline__ float exp_of(float v) { return __builtin_amdgcn_exp2f(v * 1.44269504088896340736f); }
+__device__ __forceinline__ float logistic(float v) { return __builtin_amdgcn_rcpf(1.0f + exp_of(-v)); }
+// Phi(-|v|), and exp(-v^2 / 2)
+__device__ __forceinline__ float normal_tail(float v, float* e) {
+    const float x = fabsf(v) * 0.70710678118654752440f, t = __builtin_amdgcn_rcpf(fmaf(0.3275911f, x, 1.0f));
+    *e = exp_of(-0.5f * v * v);
+    return 0.5f * *e * t * fmaf(t, fmaf(t, fmaf(t, fmaf(t, 1.061405429f, -1.453152027f), 1.421413741f), -0.284496736f), 0.254829592f);
+}
 __device__ __forceinline__ float act_value(float v, int act) {
-    if (act == SRIGL_ACT_SILU) return v / (1.0f + expf(-v));
-    if (act == SRIGL_ACT_RELU) return v < 0.0f ? 0.0f : v;   // (what is no number stays none)
-    return apply_act(v, act);
+    if (act == SRIGL_ACT_SILU) return v * logistic(v);
+    if (act == SRIGL_ACT_RELU) return v < 0.0f ? 0.0f : v;
+    if (act == SRIGL_ACT_GELU) {
+        float e;
+        const float q = normal_tail(v, &e);
+        return v * (v < 0.0f ? q : 1.0f - q);
+    }
+    return v;
 }
 __device__ __forceinline__ float act_slope(float v, int act) {
     if (act == SRIGL_ACT_RELU) return v > 0.0f ? 1.0f : 0.0f;
-    if (act == SRIGL_ACT_GELU) return 0.5f * (1.0f + erff(v * 0.70710678118654752440f)) + v * expf(-0.5f * v * v) * 0.39894228040143267794f;
+    if (act == SRIGL_ACT_GELU) {
+        float e;
+        const float q = normal_tail(v, &e);
+        return (v < 0.0f ? q : 1.0f - q) + v * e * 0.39894228040143267794f;
+    }
     if (act == SRIGL_ACT_SILU) {
-        const float p = 1.0f / (1.0f + expf(-v));
+        const float p = logistic(v);
         return p * (1.0f + v * (1.0f - p));
     }
     return 1.0f;
@@ -501,6 +603,7 @@ __device__ __forceinline__ float act_slope(float v, int act) {
 // ---- kernel and launch ----
 // Sums of a part of K, [parts][M][N] (of a pair: [parts][M][2 N], the second's behind the first's)
 struct PartOut {
+    static constexpr bool kListed = false;
     float* part;
     int N;
     long long pitch;
@@ -571,13 +674,18 @@ __global__ __launch_bounds__(WGM * WGN * 64) void k_dense(OA oa, OB ob, int M, i
         else tile_as_rows<BM, BN, WGM, WGN, 4>(smem, acc, m0, n0, M, N, to);
         return;
     }
+    if constexpr (Out::kListed)
+        if (out.active) {
+            listed_as_rows<BM, BN, WGM, WGN, V>(smem, acc, m0, n0, M, out);
+            return;
+        }
     if constexpr (PAIR) pair_as_rows<BM, BN, WGM, WGN, V>(smem, acc, m0, n0, M, N, out);
     else tile_as_rows<BM, BN, WGM, WGN, V>(smem, acc, m0, n0, M, N, out);
 }
 
 template <typename T, int BM, int BN, int WGM, int WGN, int NS, bool PAIR, class OA, class OB, class Out>
 static srigl_status launch_tiles(const OA& oa, const OB& ob, int M, int N, int stages, int parts, const Out& out, float* part, hipStream_t st) {
-    constexpr size_t ring = (size_t)std::max(NS, 1) * (BM + BN) * kLineBytes, rows = rows_lds<BM, BN, WGM>(), lds = ring > rows ? ring : rows;
+    constexpr size_t ring = (size_t)std::max(NS, 1) * (BM + BN) * kLineBytes, rows = Out::kListed ? EpiLayout<BN, WGM>::BYTES : rows_lds<BM, BN, WGM>(), lds = ring > rows ? ring : rows;
     static_assert(lds <= kLdsMax, "LDS");
     constexpr int COLS = PAIR ? BN / 2 : BN;
     auto kern = k_dense<T, BM, BN, WGM, WGN, NS, PAIR, OA, OB, Out>;

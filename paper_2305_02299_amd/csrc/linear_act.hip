@@ -42,6 +42,7 @@ DensePlan plan_dense(int M, int N, int stages, bool f32, bool pair, bool direct)
 
 template <typename T, typename TY>
 struct LinearOut {
+    static constexpr bool kListed = true;
     const int32_t* active;
     int n_active;
     const float* bias;
@@ -61,6 +62,28 @@ struct LinearOut {
                 if ((unsigned)c < (unsigned)d_out) b[q] = bias[c];
             }
         }
+    }
+    __device__ bool wants_stored() const { return z != nullptr; }
+    template <int V> __device__ void stored(int m, int s, int valid, float (&v)[V]) {
+#pragma unroll
+        for (int q = 0; q < V; ++q) v[q] += b[q];
+        store_values<T, V>(z + (size_t)m * n_active + s, v, valid);
+    }
+    template <int V> __device__ void gap_values(int gaps, float (&flat)[V]) const {
+#pragma unroll
+        for (int q = 0; q < V; ++q)
+            if (gaps >> q & 1) flat[q] = act_value(flat[q], act);
+    }
+    template <int V> __device__ void listed(int m, int c, int first, int valid, float (&v)[V], int gaps, const float (&flat)[V]) const {
+        const size_t at = (size_t)m * d_out + c;
+        float r[V] = {};
+        if (residual) load_values<TY, V>(residual + at, r, valid, first);
+#pragma unroll
+        for (int q = 0; q < V; ++q) {
+            v[q] = gaps >> q & 1 ? flat[q] : act_value(v[q], act);
+            if (residual) v[q] += r[q];
+        }
+        store_values<TY, V>(y + at, v, valid, first);
     }
     // the ablated columns lo .. hi - 1
     __device__ void ablated(int m, int lo, int hi) {
@@ -104,6 +127,7 @@ struct LinearOut {
 
 template <typename T>
 struct GatedOut {
+    static constexpr bool kListed = false;
     const float *bias_g, *bias_u;
     int n;
     T *h, *g, *u;   // g and u: nullptr where the caller does not keep them

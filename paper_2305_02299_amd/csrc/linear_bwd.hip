@@ -6,6 +6,7 @@
 // dz stands in the workspace with its rows padded by zeros to whole stages of K: the gated block's dg and du lie side by side, so that dx is one
 // product over both matrices' lines and the weight gradients are one product too.
 #include "dense_tile.h"
+#include <type_traits>
 
 namespace srigl {
 
@@ -23,71 +24,136 @@ __device__ __forceinline__ int place_of(const int32_t* active, int n_active, int
     return lo;
 }
 
-// dz[B][pitch] (pitch = padded n_active) and, per chunk of rows, the column sums of dz (ablated columns: of dy) in sums[chunk][d_out].
-template <typename T, typename TY>
-__global__ __launch_bounds__(256) void k_dz_linear(const TY* __restrict__ dy, const T* __restrict__ z, const int32_t* __restrict__ active, int n_active, int B,
-                                                  int d_out, int act, T* __restrict__ dz, int pitch, float* __restrict__ sums, int rows) {
-    const int c = blockIdx.x * 256 + threadIdx.x, m0 = blockIdx.y * rows, m1 = min(m0 + rows, B);
-    if (c >= d_out) {   // behind the last column: the padding, if the columns reach so far
-        const int s = n_active + (c - d_out);
-        if (s < pitch)
-            for (int m = m0; m < m1; ++m) dz[(size_t)m * pitch + s] = 0;
-        return;
-    }
-    int s = c;
-    bool stored = c < n_active;
-    if (active) {
-        s = place_of(active, n_active, c);
-        stored = s < n_active && active[s] == c;
-    }
-    float sum = 0.0f;
-    for (int m = m0; m < m1; ++m) {
-        float v = to_float(dy[(size_t)m * d_out + c]);
-        if (stored) {
-            if (act != SRIGL_ACT_NONE) v *= act_slope(to_float(z[(size_t)m * n_active + s]), act);
-            if (dz) dz[(size_t)m * pitch + s] = from_float<T>(v);
+// One pass over the rows of the incoming gradient.  A workgroup takes 32 groups of V = 16 / sizeof(T) consecutive columns and a chunk of rows, eight rows side by side; the column sums of
+// its eight row lanes meet in the LDS, and a chunk leaves one sum a column (no atomics: the order is fixed).  Bound by memory: three reads and two writes of 16 bytes a thread and row in the gated form;
+// one column a thread and 2-byte accesses took 229 us on 2048 x 16384 bf16.
+constexpr int kDzCols = 32, kDzRows = 8;
+
+template <int V>
+__device__ __forceinline__ void sum_row_lanes(float (*held)[kDzCols * V], float (&v)[V]) {
+    const int cg = threadIdx.x % kDzCols, rl = threadIdx.x / kDzCols;
+    __syncthreads();
+#pragma unroll
+    for (int q = 0; q < V; ++q) held[rl][q * kDzCols + cg] = v[q];
+    __syncthreads();
+    if (rl == 0)
+#pragma unroll
+        for (int q = 0; q < V; ++q)
+#pragma unroll
+            for (int r = 1; r < kDzRows; ++r) v[q] += held[r][q * kDzCols + cg];
+}
+
+// dz[B][pitch] (pitch: n_active padded with zeros) and, per chunk of rows, the sums of its columns in sums[chunk][d_out] at the neurons' columns.  dz or sums: nullptr where not wanted.
+template <typename T, typename TY, bool LISTED>
+__global__ __launch_bounds__(256) void k_dz_linear(const TY* __restrict__ dy, const T* __restrict__ z, const int32_t* __restrict__ active, int n, int B, int d_out, int act,
+                                                  T* __restrict__ dz, int pitch, float* __restrict__ sums, int rows) {
+    constexpr int V = kPiece<T>;
+    __shared__ float held[kDzRows][kDzCols * V];
+    const int s = (int)((blockIdx.x * (unsigned)kDzCols + threadIdx.x % kDzCols) * V), m0 = blockIdx.y * rows, m1 = min(m0 + rows, B), valid = n - s;
+    int col[V];
+    if constexpr (LISTED)
+#pragma unroll
+        for (int q = 0; q < V; ++q) {
+            col[q] = q < valid ? active[s + q] : -1;
+            if ((unsigned)col[q] >= (unsigned)d_out) col[q] = -1;
         }
-        sum += v;
-    }
-    if (sums) sums[(size_t)blockIdx.y * d_out + c] = sum;
+    float sum[V] = {};
+    if (s < pitch)
+        for (int m = m0 + threadIdx.x / kDzCols; m < m1; m += kDzRows) {
+            float v[V] = {}, zv[V] = {};
+            if (valid > 0) {
+                if constexpr (LISTED)
+#pragma unroll
+                    for (int q = 0; q < V; ++q) v[q] = col[q] >= 0 ? to_float(dy[(size_t)m * d_out + col[q]]) : 0.0f;
+                else load_values<TY, V>(dy + (size_t)m * d_out + s, v, valid);
+                if (act != SRIGL_ACT_NONE) {
+                    load_values<T, V>(z + (size_t)m * n + s, zv, valid);
+#pragma unroll
+                    for (int q = 0; q < V; ++q) v[q] = q < valid ? v[q] * act_slope(zv[q], act) : 0.0f;
+                }
+            }
+#pragma unroll
+            for (int q = 0; q < V; ++q) sum[q] += v[q];
+            if (dz) store_values<T, V>(dz + (size_t)m * pitch + s, v, V);
+        }
+    if (!sums) return;
+    sum_row_lanes<V>(held, sum);
+    if (threadIdx.x / kDzCols == 0)
+#pragma unroll
+        for (int q = 0; q < V; ++q) {
+            const int c = LISTED ? (q < valid ? col[q] : -1) : (q < valid ? s + q : -1);
+            if (c >= 0) sums[(size_t)blockIdx.y * d_out + c] = sum[q];
+        }
+}
+
+// The same chunks' sums of dy in the ablated columns
+template <typename TY>
+__global__ __launch_bounds__(256) void k_ablated_sums(const TY* __restrict__ dy, const int32_t* __restrict__ active, int n, int B, int d_out, float* __restrict__ sums, int rows) {
+    const int c = blockIdx.x * 256 + threadIdx.x, m0 = blockIdx.y * rows, m1 = min(m0 + rows, B);
+    if (c >= d_out) return;
+    const int s = n ? place_of(active, n, c) : 0;
+    if (s < n && active[s] == c) return;
+    float v = 0.0f;
+#pragma unroll 8
+    for (int m = m0; m < m1; ++m) v += to_float(dy[(size_t)m * d_out + c]);
+    sums[(size_t)blockIdx.y * d_out + c] = v;
 }
 
 // (dg | du)[B][2 pitch] and the column sums of both in sums[chunk][2 n]
 template <typename T>
 __global__ __launch_bounds__(256) void k_dz_gated(const T* __restrict__ dh, const T* __restrict__ g, const T* __restrict__ u, int n, int B, int act, T* __restrict__ dz,
                                                  int pitch, float* __restrict__ sums, int rows) {
-    const int c = blockIdx.x * 256 + threadIdx.x, m0 = blockIdx.y * rows, m1 = min(m0 + rows, B);
-    if (c >= pitch) return;
-    float sg = 0.0f, su = 0.0f;
-    for (int m = m0; m < m1; ++m) {
-        float dg = 0.0f, du = 0.0f;
-        if (c < n) {
-            const size_t at = (size_t)m * n + c;
-            const float d = to_float(dh[at]), gv = to_float(g[at]);
-            dg = d * to_float(u[at]) * act_slope(gv, act);
-            du = d * act_value(gv, act);
+    constexpr int V = kPiece<T>;
+    __shared__ float held[kDzRows][kDzCols * V];
+    const int c = (int)((blockIdx.x * (unsigned)kDzCols + threadIdx.x % kDzCols) * V), m0 = blockIdx.y * rows, m1 = min(m0 + rows, B), valid = n - c;
+    float sg[V] = {}, su[V] = {};
+    if (c < pitch)
+        for (int m = m0 + threadIdx.x / kDzCols; m < m1; m += kDzRows) {
+            float d[V] = {}, gv[V] = {}, uv[V] = {};
+            if (valid > 0) {
+                const size_t at = (size_t)m * n + c;
+                load_values<T, V>(dh + at, d, valid);
+                load_values<T, V>(g + at, gv, valid);
+                load_values<T, V>(u + at, uv, valid);
+#pragma unroll
+                for (int q = 0; q < V; ++q) {
+                    const float dg = d[q] * uv[q] * act_slope(gv[q], act), du = d[q] * act_value(gv[q], act);
+                    gv[q] = q < valid ? dg : 0.0f;
+                    uv[q] = q < valid ? du : 0.0f;
+                    sg[q] += gv[q];
+                    su[q] += uv[q];
+                }
+            }
+            T* const to = dz + (size_t)m * 2 * pitch + c;
+            store_values<T, V>(to, gv, V);
+            store_values<T, V>(to + pitch, uv, V);
         }
-        T* const to = dz + (size_t)m * 2 * pitch + c;
-        to[0] = from_float<T>(dg);
-        to[pitch] = from_float<T>(du);
-        sg += dg;
-        su += du;
-    }
-    if (sums && c < n) {
-        sums[(size_t)blockIdx.y * 2 * n + c] = sg;
-        sums[(size_t)blockIdx.y * 2 * n + n + c] = su;
+    if (!sums) return;
+    sum_row_lanes<V>(held, sg);
+    sum_row_lanes<V>(held, su);
+    if (threadIdx.x / kDzCols == 0 && valid > 0) {
+        float* const to = sums + (size_t)blockIdx.y * 2 * n + c;
+        store_values<float, V>(to, sg, valid);
+        store_values<float, V>(to + n, su, valid);
     }
 }
 
-// Bias gradients from the chunks' sums, in ascending order; columns [0, n) to first, [n, 2 n) to second (a layer: all to first, ablated columns times the slope at their bias)
+// Bias gradients from the chunks' sums: four lanes take every fourth chunk of a column each.  Columns [0, n) to first, [n, 2 n) to second (a layer: all to first, ablated
+// columns times the slope at their bias).
 __global__ __launch_bounds__(256) void k_sum_chunks(const float* __restrict__ sums, int chunks, int cols, int n, const int32_t* __restrict__ active, int n_active,
                                                    const float* __restrict__ bias, int act, float* __restrict__ first, float* __restrict__ second) {
-    const int c = blockIdx.x * 256 + threadIdx.x;
-    if (c >= cols) return;
+    __shared__ float held[4][64];
+    const int c = blockIdx.x * 64 + (threadIdx.x & 63), lane = threadIdx.x >> 6;
     float v = 0.0f;
-    for (int k = 0; k < chunks; ++k) v += sums[(size_t)k * cols + c];
+    if (c < cols)
+#pragma unroll 8
+        for (int k = lane; k < chunks; k += 4) v += sums[(size_t)k * cols + c];
+    held[lane][threadIdx.x & 63] = v;
+    __syncthreads();
+    if (lane != 0 || c >= cols) return;
+    v = (held[0][c & 63] + held[1][c & 63]) + (held[2][c & 63] + held[3][c & 63]);
     if (n_active < n) {
-        const int s = active ? place_of(active, n_active, c) : 0;
+        const int s = n_active ? place_of(active, n_active, c) : 0;
         if (!(s < n_active && active[s] == c)) v *= act_slope(bias ? bias[c] : 0.0f, act);
     }
     float* const to = c < n ? first : second;
@@ -96,6 +162,7 @@ __global__ __launch_bounds__(256) void k_sum_chunks(const float* __restrict__ su
 
 template <typename T>
 struct PlainOut {
+    static constexpr bool kListed = false;
     T* y;
     int N;
     template <int V> __device__ void start(int, int) {}
@@ -104,6 +171,7 @@ struct PlainOut {
 // Rows [0, n) to one matrix, [padded, padded + n) to a second; nullptr: not wanted
 template <typename T>
 struct TwoOut {
+    static constexpr bool kListed = false;
     T *first, *second;
     int N, n, padded;
     template <int V> __device__ void start(int, int) {}
@@ -127,9 +195,9 @@ static BwdPlan plan_bwd(int B, int d_in, long long cols, long long K, long long 
     BwdPlan p{};
     const bool f32 = elem == 4, direct = d_in % (16 / (int)elem) == 0;
 
-    // about a thousand workgroups of 256 columns, 8 rows to a thread at least
-    const long long groups = std::max(1ll, (sum_cols + 255) / 256), want = std::max(1ll, 1024 / groups);
-    long long rows = std::max<long long>(8, (B + want - 1) / want);
+    // about 2048 workgroups, two to eight rows to a thread and more only where the grid would be too large
+    const long long per_group = kDzCols * 16 / (long long)elem, groups = std::max(1ll, (cols / (dW_rows == cols ? 2 : 1) + per_group - 1) / per_group);
+    long long rows = std::min<long long>(8, std::max<long long>(2, B * groups / (2048 * kDzRows))) * kDzRows;
     rows = std::max<long long>(rows, ((long long)B + 65534) / 65535);
     p.chunk_rows = (int)std::min<long long>(rows, kMaxSide);
     p.chunks = (int)((B + (long long)p.chunk_rows - 1) / p.chunk_rows);
@@ -149,20 +217,29 @@ static srigl_status linear_bwd(const BwdPlan& p, const void* dy, const void* x, 
     const int32_t* const list = n == d_out ? nullptr : active;
     T* const dz = reinterpret_cast<T*>(ws);
     float *const sums = reinterpret_cast<float*>(ws + p.dz_bytes), *const part = reinterpret_cast<float*>(ws + p.dz_bytes + p.sum_bytes);
-    if (p.chunks > 0 && (n > 0 || dbias)) {
-        const dim3 grid((unsigned)((d_out + (long long)pitch - n + 255) / 256), (unsigned)p.chunks);
-        hipLaunchKernelGGL((k_dz_linear<T, TY>), grid, dim3(256), 0, st, (const TY*)dy, (const T*)z, list, n, B, d_out, act, n > 0 ? dz : nullptr, pitch,
-                           dbias ? sums : nullptr, p.chunk_rows);
+    // without an activation or ablated neurons dz is dy: only its column sums are left to do
+    const bool as_it_is = std::is_same<T, TY>::value && act == SRIGL_ACT_NONE && !list && n % kPiece<T> == 0 && !astray(16, {dy});
+    if (p.chunks > 0 && n > 0 && (!as_it_is || dbias)) {
+        const dim3 grid((unsigned)((pitch + kDzCols * kPiece<T> - 1) / (kDzCols * kPiece<T>)), (unsigned)p.chunks);
+        T* const to = as_it_is ? nullptr : dz;
+        if (list) hipLaunchKernelGGL((k_dz_linear<T, TY, true>), grid, dim3(256), 0, st, (const TY*)dy, (const T*)z, list, n, B, d_out, act, to, pitch, dbias ? sums : nullptr, p.chunk_rows);
+        else hipLaunchKernelGGL((k_dz_linear<T, TY, false>), grid, dim3(256), 0, st, (const TY*)dy, (const T*)z, list, n, B, d_out, act, to, pitch, dbias ? sums : nullptr, p.chunk_rows);
     }
-    if (dbias) hipLaunchKernelGGL(k_sum_chunks, dim3((unsigned)((d_out + 255ll) / 256)), dim3(256), 0, st, sums, p.chunks, d_out, d_out, list, n, bias, act, dbias, nullptr);
+    if (dbias) {
+        if (p.chunks > 0 && n < d_out)
+            hipLaunchKernelGGL(k_ablated_sums<TY>, dim3((unsigned)((d_out + 255ll) / 256), (unsigned)p.chunks), dim3(256), 0, st, (const TY*)dy, list, n, B, d_out, sums, p.chunk_rows);
+        hipLaunchKernelGGL(k_sum_chunks, dim3((unsigned)((d_out + 63ll) / 64)), dim3(256), 0, st, sums, p.chunks, d_out, d_out, list, n, bias, act, dbias, nullptr);
+    }
+    const T* const d = as_it_is ? (const T*)dy : dz;
+    const int d_pitch = as_it_is ? n : pitch;
     srigl_status rc = hip_ok(hipGetLastError());
     if (rc == SRIGL_OK && dx) {
-        const RowsOf<T> a{dz, pitch, B - 1, pitch};
+        const RowsOf<T> a{d, d_pitch, B - 1, d_pitch};
         const ColsOf<T> w{(const T*)Wd, d_in, d_in, n};
         rc = launch_dense<T, false>(a, w, B, d_in, stages_of<T>(n), p.dx, PlainOut<T>{(T*)dx, d_in}, part, st);
     }
     if (rc == SRIGL_OK && dWd) {
-        const ColsOf<T> a{dz, pitch, pitch, B}, b{(const T*)x, d_in, d_in, B};
+        const ColsOf<T> a{d, d_pitch, d_pitch, B}, b{(const T*)x, d_in, d_in, B};
         rc = launch_dense<T, false>(a, b, n, d_in, stages_of<T>(B), p.dW, PlainOut<T>{(T*)dWd, d_in}, part, st);
     }
     return rc;
@@ -176,10 +253,10 @@ static srigl_status gated_bwd(const BwdPlan& p, const void* dh, const void* x, i
     float *const sums = reinterpret_cast<float*>(ws + p.dz_bytes), *const part = reinterpret_cast<float*>(ws + p.dz_bytes + p.sum_bytes);
     const bool want_sums = dbias_g || dbias_u;
     if (p.chunks > 0 && n > 0)
-        hipLaunchKernelGGL(k_dz_gated<T>, dim3((unsigned)((pitch + 255) / 256), (unsigned)p.chunks), dim3(256), 0, st, (const T*)dh, (const T*)g, (const T*)u, n, B, act, dz,
+        hipLaunchKernelGGL(k_dz_gated<T>, dim3((unsigned)((pitch + kDzCols * kPiece<T> - 1) / (kDzCols * kPiece<T>)), (unsigned)p.chunks), dim3(256), 0, st, (const T*)dh, (const T*)g, (const T*)u, n, B, act, dz,
                            pitch, want_sums ? sums : nullptr, p.chunk_rows);
     if (want_sums && n > 0)
-        hipLaunchKernelGGL(k_sum_chunks, dim3((unsigned)((2ll * n + 255) / 256)), dim3(256), 0, st, sums, p.chunks, 2 * n, n, nullptr, n, nullptr, act, dbias_g, dbias_u);
+        hipLaunchKernelGGL(k_sum_chunks, dim3((unsigned)((2ll * n + 63) / 64)), dim3(256), 0, st, sums, p.chunks, 2 * n, n, nullptr, n, nullptr, act, dbias_g, dbias_u);
     srigl_status rc = hip_ok(hipGetLastError());
     if (rc == SRIGL_OK && dx) {
         const RowsOf<T> a{dz, 2ll * pitch, B - 1, 2 * pitch};
