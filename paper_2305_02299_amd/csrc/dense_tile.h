@@ -614,26 +614,32 @@ struct PartOut {
         store_values<float, V>(part + (size_t)m * pitch + N + c, w, valid);
     }
 };
+// (eight parts' values are requested together: a thread waits for memory once or twice)
 template <class Out, int V, bool PAIR>
 __global__ __launch_bounds__(256) void k_dense_join(const float* __restrict__ part, int parts, int M, int N, Out out) {
+    constexpr int TOGETHER = 8;
     const int c = (blockIdx.x * 256 + threadIdx.x) * V, valid = N - c;
     if (valid <= 0) return;
     out.template start<V>(c, valid);
     const long long pitch = PAIR ? 2ll * N : N;
     for (int m = blockIdx.y; m < M; m += gridDim.y) {
         float v[V] = {}, w[V] = {};
-#pragma unroll 4
-        for (int z = 0; z < parts; ++z) {
-            const float* const p = part + ((size_t)z * M + m) * pitch + c;
-            float t[V];
-            load_values<float, V>(p, t, valid);
+        for (int z0 = 0; z0 < parts; z0 += TOGETHER) {
+            float t[TOGETHER][V] = {}, u[TOGETHER][V] = {};
 #pragma unroll
-            for (int q = 0; q < V; ++q) v[q] += t[q];
-            if constexpr (PAIR) {
-                load_values<float, V>(p + N, t, valid);
-#pragma unroll
-                for (int q = 0; q < V; ++q) w[q] += t[q];
+            for (int k = 0; k < TOGETHER; ++k) {
+                const float* const p = part + ((size_t)min(z0 + k, parts - 1) * M + m) * pitch + c;
+                load_values<float, V>(p, t[k], valid);
+                if constexpr (PAIR) load_values<float, V>(p + N, u[k], valid);
             }
+#pragma unroll
+            for (int k = 0; k < TOGETHER; ++k)
+                if (z0 + k < parts)
+#pragma unroll
+                    for (int q = 0; q < V; ++q) {
+                        v[q] += t[k][q];
+                        if constexpr (PAIR) w[q] += u[k][q];
+                    }
         }
         if constexpr (PAIR) out.template row<V>(m, c, valid, v, w);
         else out.template row<V>(m, c, valid, v);
@@ -695,8 +701,12 @@ static srigl_status launch_tiles(const OA& oa, const OB& ob, int M, int N, int s
     if (n_wg > 0x7fffffffll || parts < 1 || parts > 65535) return SRIGL_ERR_UNSUPPORTED;
     hipLaunchKernelGGL(kern, dim3((unsigned)n_wg, (unsigned)parts), dim3(WGM * WGN * 64), lds, st, oa, ob, M, N, stages, parts, out, part);
     if (parts > 1) {
-        const dim3 grid((unsigned)((N + 1023ll) / 1024), (unsigned)std::min(M, 65535));
-        hipLaunchKernelGGL((k_dense_join<Out, 4, PAIR>), grid, dim3(256), 0, st, part, parts, M, N, out);
+        bool one = false;   // a neuron to a thread, which writes the ablated columns in front of its own too
+        if constexpr (Out::kListed) one = out.active != nullptr;
+        const dim3 grid((unsigned)(one ? (N + 255ll) / 256 : (N + 1023ll) / 1024), (unsigned)std::min(M, 65535));
+        if constexpr (Out::kListed)
+            if (one) hipLaunchKernelGGL((k_dense_join<Out, 1, PAIR>), grid, dim3(256), 0, st, part, parts, M, N, out);
+        if (!one) hipLaunchKernelGGL((k_dense_join<Out, 4, PAIR>), grid, dim3(256), 0, st, part, parts, M, N, out);
     }
     return hip_ok(hipGetLastError());
 }
@@ -722,6 +732,109 @@ static srigl_status launch_dense(const OA& oa, const OB& ob, int M, int N, int s
     }
     if (plan.tile != kTileS) return launch_tiles<T, 128, 128, 2, 2, 4, PAIR>(oa, ob, M, N, stages, plan.parts, out, part, st);
     return launch_tiles<T, 64, SN, 2, 2, 4, PAIR>(oa, ob, M, N, stages, plan.parts, out, part, st);
+}
+// ---- few rows of x ----
+// Products with at most 64 rows of x are bound by reading the weights.  A workgroup takes 16 neurons (of a pair: of both matrices) and all of K, its wavefronts 128 bytes of the lines in turn, straight
+// from memory into the matrix units' registers: v_mfma_f32_16x16x32_bf16 with lane l holding row l % 16, k = 8 (l / 16) .. + 7 (fp32: 16x16x4, k = 4 (l / 16) + j in the j-th of four),
+// neurons against 16 rows of x, so that a batch of one costs what 16 do.  The wavefronts' sums meet in the LDS: no second launch.
+typedef float f32x4_acc_t __attribute__((ext_vector_type(4)));
+__device__ __forceinline__ void few_mma(f32x4_acc_t& acc, const uint4& a, const uint4& b, uint16_t) {
+    acc = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8_t, a), __builtin_bit_cast(bf16x8_t, b), acc, 0, 0, 0);
+}
+__device__ __forceinline__ void few_mma(f32x4_acc_t& acc, const uint4& a, const uint4& b, float) {
+    acc = __builtin_amdgcn_mfma_f32_16x16x4f32(__uint_as_float(a.x), __uint_as_float(b.x), acc, 0, 0, 0);
+    acc = __builtin_amdgcn_mfma_f32_16x16x4f32(__uint_as_float(a.y), __uint_as_float(b.y), acc, 0, 0, 0);
+    acc = __builtin_amdgcn_mfma_f32_16x16x4f32(__uint_as_float(a.z), __uint_as_float(b.z), acc, 0, 0, 0);
+    acc = __builtin_amdgcn_mfma_f32_16x16x4f32(__uint_as_float(a.w), __uint_as_float(b.w), acc, 0, 0, 0);
+}
+
+// NB: blocks of 16 rows of x; UNITS of 128 bytes of a line requested together
+template <typename T, int NB, int NW, bool PAIR, int UNITS, class Out>
+__global__ __launch_bounds__(NW * 64) void k_dense_few(const T* __restrict__ x, int B, int K, const T* __restrict__ W, long long to_second, int n, int rows, Out out) {
+    constexpr int MATS = PAIR ? 2 : 1, STEP = 64 / (int)sizeof(T), UNIT = 2 * STEP, P = kPiece<T>;
+    __shared__ float sums[NW][MATS][16][17];   // [neuron][row of x], of 16 rows of x at a time
+    const int lane = threadIdx.x & 63, wv = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), s0 = blockIdx.x * rows;
+    const T *w[MATS], *xr[NB];
+    const int off = (lane >> 4) * P;
+    w[0] = W + (size_t)min(s0 + min(lane & 15, rows - 1), n - 1) * K + off;
+    if constexpr (PAIR) w[1] = reinterpret_cast<const T*>(reinterpret_cast<const unsigned char*>(w[0]) + to_second);
+#pragma unroll
+    for (int b = 0; b < NB; ++b) xr[b] = x + (size_t)min(b * 16 + (lane & 15), B - 1) * K + off;
+    f32x4_acc_t acc[MATS][NB] = {};
+    const int units = K / UNIT;
+    auto compute = [&](int first, int count, auto load) {
+        uint4 wp[MATS][UNITS][2], xp[NB][UNITS][2];
+#pragma unroll
+        for (int u = 0; u < UNITS; ++u)
+            if (u < count)
+#pragma unroll
+                for (int h = 0; h < 2; ++h) {
+                    const int k = (first + u * NW) * UNIT + h * STEP;
+#pragma unroll
+                    for (int i = 0; i < MATS; ++i) wp[i][u][h] = load(w[i], k);
+#pragma unroll
+                    for (int b = 0; b < NB; ++b) xp[b][u][h] = load(xr[b], k);
+                }
+#pragma unroll
+        for (int u = 0; u < UNITS; ++u)
+            if (u < count)
+#pragma unroll
+                for (int h = 0; h < 2; ++h)
+#pragma unroll
+                    for (int i = 0; i < MATS; ++i)
+#pragma unroll
+                        for (int b = 0; b < NB; ++b) few_mma(acc[i][b], wp[i][u][h], xp[b][u][h], T{});
+    };
+    const auto whole_piece = [&](const T* p, int k) { return load_piece(p + k, P); };
+    for (int u = wv; u < units; u += NW * UNITS) compute(u, (units - u + NW - 1) / NW, whole_piece);
+    if (K % UNIT && wv == units % NW) compute(units, 1, [&](const T* p, int k) { return load_piece(p + k, K - k - off); });
+    const int s = threadIdx.x & 15, r = threadIdx.x >> 4;   // 256 threads write
+    if (s < rows && s0 + s < n) out.template start<1>(s0 + s, 1);
+#pragma unroll
+    for (int b = 0; b < NB; ++b) {
+        if (b > 0) __syncthreads();
+#pragma unroll
+        for (int i = 0; i < MATS; ++i)
+#pragma unroll
+            for (int e = 0; e < 4; ++e) sums[wv][i][4 * (lane >> 4) + e][lane & 15] = acc[i][b][e];
+        __syncthreads();
+        const int m = 16 * b + r;
+        if (r >= 16 || s >= rows || s0 + s >= n || m >= B) continue;
+        float v[1] = {}, u[1] = {};
+#pragma unroll
+        for (int k = 0; k < NW; ++k) {
+            v[0] += sums[k][0][s][r];
+            if constexpr (PAIR) u[0] += sums[k][1][s][r];
+        }
+        if constexpr (PAIR) out.template row<1>(m, s0 + s, 1, v, u);
+        else out.template row<1>(m, s0 + s, 1, v);
+    }
+}
+
+// Whether the products of B rows of x with lines of K elements run here: up to 16 rows always, more while x, which every workgroup reads again, is short (`units` of 128 bytes a line).  us, weights out of
+// HBM, here against tiles: bf16 4096 -> 16384 at 1 row 24.8 and 34.4, at 16 31.9 and 32.6, at 32 45.8 and 32.5; 1024 -> 1024 at 32 4.6 and 7.3, at 64 7.1 and 8.0; gated 4096 -> 4096 at 32 17.5 and
+// 19.3, at 64 26.5 and 21.4; fp32 3072 -> 768 at 16 11.2 and 12.4, at 32 16.9 and 12.7; 1001 -> 777 (pieces that begin anywhere) at 32 7.5 and 8.2, at 64 12.1 and 9.0.
+inline bool few_rows(int B, int K, bool f32, bool pair) {
+    const long long units = (long long)K * (f32 ? 4 : 2) / 128;
+    return B <= 16 || (B <= 32 && units <= (pair ? 64 : 48)) || (B <= 64 && units <= (pair ? 24 : 16) && K % (f32 ? 4 : 8) == 0);
+}
+template <typename T, bool PAIR, class Out>
+static srigl_status launch_few(const T* x, int B, int K, const T* W, long long to_second, int n, const Out& out, hipStream_t st) {
+    // Few neurons: four of them to a workgroup (the others' places in the matrix units repeat the last one), since a compute unit alone brings in little: bf16 3072 -> 768 at one row 4.6 us against 5.8 with
+    // 16, 1024 -> 1024 2.7 and 3.0, but 768 -> 3072 3.9 and 3.2.
+    const int rows = n >= 2048 ? 16 : 4;
+    const dim3 grid((unsigned)((n + (long long)rows - 1) / rows));
+    const bool wide = (long long)K * (int)sizeof(T) >= 20 * 128;   // eight wavefronts to a line, else four (bf16 4096 -> 16384 at one row 24.8 us, 27.3 with four)
+#define SRIGL_FEW(NB, UNITS) \
+    do { \
+        if (wide) hipLaunchKernelGGL((k_dense_few<T, NB, 8, PAIR, UNITS, Out>), grid, dim3(512), 0, st, x, B, K, W, to_second, n, rows, out); \
+        else hipLaunchKernelGGL((k_dense_few<T, NB, 4, PAIR, UNITS, Out>), grid, dim3(256), 0, st, x, B, K, W, to_second, n, rows, out); \
+    } while (0)
+    if (B <= 16) SRIGL_FEW(1, 4);
+    else if (B <= 32) SRIGL_FEW(2, PAIR ? 2 : 3);
+    else SRIGL_FEW(4, 2);
+#undef SRIGL_FEW
+    return hip_ok(hipGetLastError());
 }
 template <typename T> inline int stages_of(long long K) { return (int)((K + kStageK<T> - 1) / kStageK<T>); }
 

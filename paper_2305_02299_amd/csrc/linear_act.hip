@@ -178,7 +178,8 @@ template <typename T, typename TY>
 static srigl_status linear_act(const void* x, int B, int d_in, const void* Wd, const int32_t* active, int n, const float* bias, const void* residual, int d_out,
                                void* y, void* z, int act, void* ws, size_t ws_bytes, hipStream_t st) {
     const DensePlan plan = plan_forward(B, d_in, n, sizeof(T) == 4, false);
-    if (!scratch_fits(ws, ws_bytes, part_bytes(plan, B, n, false))) return SRIGL_ERR_CAPACITY;
+    const bool few = few_rows(B, d_in, sizeof(T) == 4, false);
+    if (!few && !scratch_fits(ws, ws_bytes, part_bytes(plan, B, n, false))) return SRIGL_ERR_CAPACITY;
     if (n == 0) {
         hipLaunchKernelGGL(k_bias_rows<TY>, dim3((unsigned)((d_out + 255) / 256), (unsigned)std::min(B, 65535)), dim3(256), 0, st, bias, (const TY*)residual, B, d_out,
                            (TY*)y, act);
@@ -186,6 +187,7 @@ static srigl_status linear_act(const void* x, int B, int d_in, const void* Wd, c
     }
     const RowsOf<T> a{(const T*)x, d_in, B - 1, d_in}, w{(const T*)Wd, d_in, n - 1, d_in};
     const LinearOut<T, TY> out{n == d_out ? nullptr : active, n, bias, (const TY*)residual, d_out, (TY*)y, (T*)z, act, {}};
+    if (few) return launch_few<T, false>((const T*)x, B, d_in, (const T*)Wd, 0, n, out, st);
     return launch_dense<T, false>(a, w, B, n, stages_of<T>(d_in), plan, out, (float*)ws, st);
 }
 
@@ -193,10 +195,12 @@ template <typename T>
 static srigl_status gated(const void* x, int B, int d_in, const void* Wg, const void* Wu, int n, const float* bias_g, const float* bias_u, int act, void* h, void* g,
                           void* u, void* ws, size_t ws_bytes, hipStream_t st) {
     const DensePlan plan = plan_forward(B, d_in, n, sizeof(T) == 4, true);
-    if (!scratch_fits(ws, ws_bytes, part_bytes(plan, B, n, true))) return SRIGL_ERR_CAPACITY;
+    const bool few = few_rows(B, d_in, sizeof(T) == 4, true);
+    if (!few && !scratch_fits(ws, ws_bytes, part_bytes(plan, B, n, true))) return SRIGL_ERR_CAPACITY;
     const RowsOf<T> a{(const T*)x, d_in, B - 1, d_in};
     const PairedRows<T, 32> w{(const T*)Wg, bytes_between(Wg, Wu), d_in, n - 1, d_in};
     const GatedOut<T> out{bias_g, bias_u, n, (T*)h, (T*)g, (T*)u, act, {}, {}};
+    if (few) return launch_few<T, true>((const T*)x, B, d_in, (const T*)Wg, bytes_between(Wg, Wu), n, out, st);
     return launch_dense<T, true>(a, w, B, n, stages_of<T>(d_in), plan, out, (float*)ws, st);
 }
 
@@ -208,7 +212,7 @@ extern "C" {
 
 size_t srigl_structured_act_workspace_bytes(int32_t B, int32_t d_in, int32_t n_active, srigl_dtype dtype) {
     if (B < 0 || d_in < 0 || n_active < 0 || B > kMaxSide || d_in > kMaxSide || n_active > kMaxSide || !known_dtype(dtype)) return 0;
-    return part_bytes(plan_forward(B, d_in, n_active, dtype == SRIGL_F32, false), B, n_active, false);
+    return few_rows(B, d_in, dtype == SRIGL_F32, false) ? 0 : part_bytes(plan_forward(B, d_in, n_active, dtype == SRIGL_F32, false), B, n_active, false);
 }
 
 srigl_status srigl_structured_linear_fwd_act(const void* x, srigl_dtype x_dtype, int32_t B, int32_t d_in, const void* Wd, srigl_dtype w_dtype, const int32_t* active,
@@ -230,7 +234,7 @@ srigl_status srigl_structured_linear_fwd_act(const void* x, srigl_dtype x_dtype,
 
 size_t srigl_gated_workspace_bytes(int32_t B, int32_t d_in, int32_t n, srigl_dtype dtype) {
     if (B < 0 || d_in < 0 || n < 0 || B > kMaxSide || d_in > kMaxSide || n > kMaxSide || !known_dtype(dtype)) return 0;
-    return part_bytes(plan_forward(B, d_in, n, dtype == SRIGL_F32, true), B, n, true);
+    return few_rows(B, d_in, dtype == SRIGL_F32, true) ? 0 : part_bytes(plan_forward(B, d_in, n, dtype == SRIGL_F32, true), B, n, true);
 }
 
 srigl_status srigl_gated_linear_fwd(const void* x, srigl_dtype x_dtype, int32_t B, int32_t d_in, const void* Wg, const void* Wu, srigl_dtype w_dtype, int32_t n,
