@@ -47,6 +47,8 @@ template <typename T, int V> struct AnyPlace { typedef T type __attribute__((ext
 // line(l, first, valid): where elements first .. of line l begin, *valid how many of them there are (<= 0: none).
 // For loads that go straight into the LDS, of operands whose lines begin at and are multiples of 16 bytes: stage(h, l) is the scalar address that lane_offset(l, first) bytes are
 // added to (l: any line of the 1 KB that the wavefront's load fills, whose lines are of one matrix), with lines and columns past the last one at the last one.
+// inside(h): every piece of stage h can be read as 16 bytes (lines along K: all of its K is there; across K: a piece may reach into the line behind, whose values
+// go to columns that nobody stores, so all but the matrix's last line).
 // Stages by number: whole() of them have all of their K, the i-th of these being stage index(i); of tails() others, stage tail(t), a part lies behind the end of K.
 // Along K: line = tile row, elements = k.
 template <typename T> struct RowsOf {
@@ -58,6 +60,7 @@ template <typename T> struct RowsOf {
     __device__ const T* line(int l, int first, int* valid) const { *valid = K - first; return base + (size_t)min(l, last) * pitch + first; }
     __device__ const unsigned char* stage(int h, int) const { return reinterpret_cast<const unsigned char*>(base) + (size_t)h * kLineBytes; }
     __device__ uint32_t lane_offset(int l, int first) const { return ((uint32_t)min(l, last) * (uint32_t)pitch + first) * (uint32_t)sizeof(T); }
+    __device__ bool inside(int h) const { return (h + 1) * kStageK<T> <= K; }
     bool direct(int lines) const { return direct_rows(base, pitch, lines) && K % kPiece<T> == 0; }
     __device__ int whole() const { return K / kStageK<T>; }
     __device__ int index(int i) const { return i; }
@@ -83,6 +86,7 @@ template <typename T, int HALF> struct PairedRows {
     __device__ uint32_t lane_offset(int l, int first) const {
         return ((uint32_t)min((l / HALF >> 1) * HALF + l % HALF, last) * (uint32_t)pitch + first) * (uint32_t)sizeof(T);
     }
+    __device__ bool inside(int h) const { return (h + 1) * kStageK<T> <= K; }
     bool direct(int lines) const { return direct_rows(base, pitch, lines) && to_second % 16 == 0 && K % kPiece<T> == 0; }
     __device__ int whole() const { return K / kStageK<T>; }
     __device__ int index(int i) const { return i; }
@@ -99,6 +103,7 @@ template <typename T> struct ColsOf {
     __device__ const T* line(int l, int first, int* valid) const { *valid = l < K ? cols - first : 0; return base + (size_t)l * pitch + first; }
     __device__ const unsigned char* stage(int h, int) const { return reinterpret_cast<const unsigned char*>(base + (size_t)h * kStageK<T> * pitch); }
     __device__ uint32_t lane_offset(int l, int first) const { return ((uint32_t)l * (uint32_t)pitch + min(first, cols - kPiece<T>)) * (uint32_t)sizeof(T); }
+    __device__ bool inside(int h) const { return (h + 1) * kStageK<T> < K && pitch >= kPiece<T>; }
     bool direct(int) const { return direct_rows(base, pitch, kStageK<T>) && cols % kPiece<T> == 0; }
     __device__ int whole() const { return K / kStageK<T>; }
     __device__ int index(int i) const { return i; }
@@ -130,6 +135,10 @@ template <typename T> struct PairedCols {
     __device__ int index(int i) const { const int w = n / kStageK<T>; return i < w ? i : i - w + padded / kStageK<T>; }
     __device__ int tails() const { return n % kStageK<T> ? 2 : 0; }
     __device__ int tail(int t) const { return n / kStageK<T> + t * (padded / kStageK<T>); }
+    __device__ bool inside(int h) const {
+        const int behind = padded / kStageK<T>;
+        return ((h < behind ? h : h - behind) + 1) * kStageK<T> < n && pitch >= kPiece<T>;
+    }
     bool direct(int) const { return direct_rows(base, pitch, kStageK<T>) && to_second % 16 == 0 && cols % kPiece<T> == 0; }
 };
 
@@ -211,13 +220,22 @@ struct RegStage {
     static constexpr int PASSES = R * kLineBytes / 16 / NT, PER_LINE = Op::kAlong ? 8 : R / kPiece<T>;
     static_assert(R * kLineBytes % (16 * NT) == 0, "pieces to a thread");
     uint4 held[PASSES];
-    __device__ void load(const Op& op, int h) {
+    __device__ __forceinline__ void load(const Op& op, int h) {
+        int valid;
+        if (op.inside(h)) {   // (one branch for all pieces: with one a piece each waited for the one before, 3 us a stage)
 #pragma unroll
-        for (int p = 0; p < PASSES; ++p) {
-            const int u = p * NT + threadIdx.x, l = u / PER_LINE, q = u % PER_LINE;
-            int valid;
-            const T* at = Op::kAlong ? op.line(l, h * kStageK<T> + q * kPiece<T>, &valid) : op.line(h * kStageK<T> + l, q * kPiece<T>, &valid);
-            held[p] = load_piece(at, valid);
+            for (int p = 0; p < PASSES; ++p) {
+                const int u = p * NT + threadIdx.x, l = u / PER_LINE, first = u % PER_LINE * kPiece<T>;
+                if constexpr (Op::kAlong) held[p] = load_piece(op.line(l, h * kStageK<T> + first, &valid), kPiece<T>);
+                else held[p] = load_piece(op.line(h * kStageK<T> + l, min(first, op.cols - 1), &valid), kPiece<T>);
+            }
+        } else {
+#pragma unroll
+            for (int p = 0; p < PASSES; ++p) {
+                const int u = p * NT + threadIdx.x, l = u / PER_LINE, first = u % PER_LINE * kPiece<T>;
+                const T* const at = Op::kAlong ? op.line(l, h * kStageK<T> + first, &valid) : op.line(h * kStageK<T> + l, first, &valid);
+                held[p] = load_piece(at, valid);
+            }
         }
     }
     __device__ void store(unsigned char* stage) const {
