@@ -732,7 +732,9 @@ static srigl_status launch_tiles(const OA& oa, const OB& ob, int M, int N, int s
 // Tile and parts of K of a product (of a pair: N neurons, two sums each)
 struct DensePlan { int tile, parts; };
 enum { kTileS = 0, kTileM = 1, kTileH = 2, kTileL = 3 };   // 64 x 64 (of a pair 64 x 128), 128 x 128, 256 x 128 and 256 x 256 (bf16, direct loads)
-DensePlan plan_dense(int M, int N, int stages, bool f32, bool pair, bool direct);
+enum DenseKind { kDenseForward = 0, kDensePair = 1, kDenseGradX = 2, kDenseGradW = 3 };   // a layer's forward product, a gated block's, gradients of x and of W
+// direct: rows are multiples of 16 bytes (a choice by sizes, so that the workspace does not depend on addresses)
+DensePlan plan_dense(DenseKind kind, int M, int N, int stages, bool f32, bool direct);
 // bytes of the parts' sums
 inline size_t part_bytes(DensePlan p, int M, int N, bool pair) { return p.parts > 1 ? (size_t)p.parts * M * N * (pair ? 2 : 1) * sizeof(float) : 0; }
 
@@ -748,7 +750,10 @@ static srigl_status launch_dense(const OA& oa, const OB& ob, int M, int N, int s
         if (plan.tile == kTileL) return launch_tiles<T, 256, 256, 2, 4, 2, PAIR>(oa, ob, M, N, stages, plan.parts, out, part, st);
         if (plan.tile == kTileH) return launch_tiles<T, 256, 128, 4, 2, 3, PAIR>(oa, ob, M, N, stages, plan.parts, out, part, st);
     }
-    if (plan.tile != kTileS) return launch_tiles<T, 128, 128, 2, 2, 4, PAIR>(oa, ob, M, N, stages, plan.parts, out, part, st);
+    // 128 x 128 by eight wavefronts (four of 64 x 64 leave each SIMD one, which waits at every barrier: bf16 512 rows, 768 -> 3072, 15.2 us, now 11.5; fp32 2048 rows, 4096 -> 4096, 513 and 496), in bf16
+    // only where both operands' lines run along K: the transposing reads of half as wide wavefronts are 1.5 times as many (gradient of W, 2048 rows, 4096 -> 4096, 83.5 us against 77.8)
+    constexpr bool EIGHT = sizeof(T) == 4 || (OA::kAlong && OB::kAlong);
+    if (plan.tile != kTileS) return launch_tiles<T, 128, 128, EIGHT && PAIR ? 4 : 2, EIGHT && !PAIR ? 4 : 2, 4, PAIR>(oa, ob, M, N, stages, plan.parts, out, part, st);
     return launch_tiles<T, 64, SN, 2, 2, 4, PAIR>(oa, ob, M, N, stages, plan.parts, out, part, st);
 }
 // ---- few rows of x ----

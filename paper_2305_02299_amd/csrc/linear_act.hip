@@ -8,32 +8,77 @@
 
 namespace srigl {
 
-// Expected time (us) of a product in a tile and `parts` parts of K: rounds of workgroups over the compute units, each a fixed part and a part per 1000 elements of K
-// (less where a workgroup has its compute unit to itself); the parts' sums are written and read and joined by a second launch.
-struct DenseModel { int bm, bn; float fixed, round, per_k, alone; int slots; };
-static const DenseModel kDenseBf16[] = {{64, 64, 2.8f, 1.1f, 5.6f, 0.65f, 512}, {128, 128, 3.1f, 3.0f, 9.3f, 1.0f, 256}, {256, 128, 1.6f, 4.7f, 10.5f, 1.0f, 256}, {256, 256, 0.7f, 7.0f, 20.2f, 1.0f, 256}};
-static const DenseModel kDenseF32[] = {{64, 64, 2.1f, 1.0f, 38.0f, 0.5f, 512}, {128, 128, 2.1f, 2.0f, 70.0f, 1.0f, 256}};
-static const DenseModel kPairBf16 = {64, 128, 2.0f, 3.0f, 5.0f, 1.0f, 256}, kPairF32 = {64, 128, 2.1f, 2.0f, 38.0f, 1.0f, 256};
-constexpr float kJoinUs = 2.5f, kPartUs = 1.8e-6f;   // a second launch; a part's sum written and read
+// Expected time (us) of a product in a tile and `parts` parts of K: a fixed part, a part a round of workgroups over the compute units and, by 1000 elements of K, a part a round and one that follows how
+// full the rounds are, a part per million results, a second launch and the parts' sums (a million of them written and read) where there are several.  Non-negative least squares on the relative error of
+// 170000 timings in graphs, every tile and 1 to 16 parts of 29000 random products (17 to 2048 rows, 100 to 4096 wide, 100 to 16384 neurons): 3 to 12 % a timing; the tile and parts of smallest time are 0.1
+// to 1.1 % behind the fastest on average by kind and type, 8 % at worst in 95 of 100, 37 % at worst.
+struct DenseModel {
+    int kind, f32, direct, tile, slots;
+    float us[7];   // fixed, round, per_k, per_k_full, results, second, part
+};
+static const DenseModel kDenseModels[] = {
+    {0, 0, 0, 0, 512, {4.47f, 1.49f, 6.49f, 4.98f, 0.904f, 2.48f, 1.67f}},
+    {0, 0, 0, 1, 512, {10.8f, 0.0f, 12.6f, 9.99f, 0.63f, 1.49f, 1.5f}},
+    {0, 0, 1, 0, 512, {3.49f, 2.7f, 2.91f, 4.71f, 0.509f, 2.0f, 2.48f}},
+    {0, 0, 1, 1, 256, {4.8f, 3.06f, 5.67f, 4.17f, 0.502f, 2.24f, 1.63f}},
+    {0, 0, 1, 2, 256, {7.47f, 2.08f, 8.42f, 5.26f, 0.699f, 2.13f, 1.48f}},
+    {0, 0, 1, 3, 256, {10.5f, 3.56f, 15.1f, 9.99f, 0.505f, 1.13f, 1.14f}},
+    {0, 1, 0, 0, 256, {5.67f, 0.0315f, 20.9f, 0.0f, 1.11f, 2.17f, 1.88f}},
+    {0, 1, 0, 1, 256, {10.2f, 0.0f, 66.2f, 2.89f, 0.684f, 0.902f, 1.5f}},
+    {0, 1, 1, 0, 256, {5.59f, 0.409f, 16.9f, 1.5f, 1.22f, 2.63f, 1.91f}},
+    {0, 1, 1, 1, 256, {6.32f, 2.1f, 56.7f, 7.6f, 0.948f, 3.35f, 1.7f}},
+    {1, 0, 0, 0, 1024, {7.51f, 0.0f, 9.0f, 21.7f, 0.416f, 2.47f, 1.7f}},
+    {1, 0, 0, 1, 512, {10.4f, 0.0f, 12.5f, 10.0f, 0.361f, 2.25f, 1.3f}},
+    {1, 0, 1, 0, 256, {3.6f, 3.77f, 4.39f, 2.74f, 0.488f, 2.62f, 1.53f}},
+    {1, 0, 1, 1, 256, {4.13f, 3.35f, 5.59f, 4.26f, 0.343f, 2.83f, 1.63f}},
+    {1, 0, 1, 2, 256, {6.5f, 2.58f, 8.5f, 4.94f, 0.55f, 2.73f, 1.46f}},
+    {1, 0, 1, 3, 256, {9.16f, 3.71f, 15.3f, 9.14f, 0.348f, 2.44f, 1.12f}},
+    {1, 1, 0, 0, 256, {6.75f, 0.0f, 36.2f, 0.0f, 0.531f, 2.66f, 1.51f}},
+    {1, 1, 0, 1, 256, {8.73f, 0.0f, 65.8f, 0.0f, 0.653f, 2.51f, 1.38f}},
+    {1, 1, 1, 0, 256, {3.88f, 3.3f, 31.4f, 5.3f, 0.807f, 3.44f, 1.57f}},
+    {1, 1, 1, 1, 256, {5.21f, 2.3f, 57.0f, 6.95f, 0.709f, 4.32f, 1.76f}},
+    {2, 0, 0, 0, 1536, {5.67f, 0.0f, 11.0f, 13.7f, 0.375f, 2.93f, 2.48f}},
+    {2, 0, 0, 1, 1536, {8.5f, 0.0f, 16.4f, 30.0f, 0.123f, 3.27f, 1.67f}},
+    {2, 0, 1, 0, 256, {7.2f, 0.119f, 3.6f, 1.06f, 0.503f, 2.87f, 2.85f}},
+    {2, 0, 1, 1, 256, {7.95f, 1.58f, 5.67f, 3.77f, 0.394f, 3.38f, 2.38f}},
+    {2, 0, 1, 2, 256, {9.2f, 0.299f, 8.67f, 4.92f, 0.479f, 3.87f, 1.88f}},
+    {2, 0, 1, 3, 256, {10.8f, 0.656f, 15.9f, 8.48f, 0.602f, 4.97f, 1.46f}},
+    {2, 1, 0, 0, 1536, {1.59f, 3.58f, 28.0f, 67.0f, 1.34f, 2.57f, 2.99f}},
+    {2, 1, 0, 1, 256, {7.69f, 0.0f, 76.2f, 0.0f, 0.777f, 4.15f, 1.17f}},
+    {2, 1, 1, 0, 256, {6.79f, 0.0f, 17.0f, 1.88f, 0.676f, 2.97f, 2.47f}},
+    {2, 1, 1, 1, 256, {8.5f, 0.0f, 57.7f, 8.49f, 0.138f, 4.35f, 2.22f}},
+    {3, 0, 0, 0, 1536, {6.62f, 0.0f, 9.87f, 18.1f, 0.397f, 2.33f, 2.54f}},
+    {3, 0, 0, 1, 768, {9.12f, 0.0f, 16.4f, 19.7f, 0.362f, 3.69f, 1.4f}},
+    {3, 0, 1, 0, 512, {5.56f, 1.34f, 3.94f, 5.76f, 0.476f, 2.8f, 2.89f}},
+    {3, 0, 1, 1, 256, {5.9f, 2.99f, 7.42f, 3.96f, 0.336f, 4.43f, 1.74f}},
+    {3, 0, 1, 2, 256, {7.05f, 1.96f, 10.5f, 7.67f, 0.35f, 5.19f, 1.39f}},
+    {3, 0, 1, 3, 256, {8.06f, 3.53f, 17.1f, 13.5f, 0.227f, 6.23f, 1.06f}},
+    {3, 1, 0, 0, 1536, {5.45f, 0.0f, 26.5f, 99.4f, 0.553f, 2.66f, 2.28f}},
+    {3, 1, 0, 1, 256, {8.31f, 0.0f, 75.8f, 1.78f, 0.473f, 4.59f, 1.09f}},
+    {3, 1, 1, 0, 256, {5.74f, 0.608f, 17.4f, 3.12f, 0.575f, 2.99f, 2.14f}},
+    {3, 1, 1, 1, 256, {6.12f, 1.75f, 58.2f, 13.0f, 0.623f, 5.07f, 1.69f}},
+};
 
-// direct: rows are multiples of 16 bytes (a choice by sizes, so that the workspace does not depend on addresses)
-DensePlan plan_dense(int M, int N, int stages, bool f32, bool pair, bool direct) {
+DensePlan plan_dense(DenseKind kind, int M, int N, int stages, bool f32, bool direct) {
     if (M <= 0 || N <= 0) return {kTileS, 1};
     struct Key { int32_t M, N, stages, form; };
     static thread_local DecisionCache<Key, DensePlan, 64> cache;
-    return cache.get(Key{M, N, stages, f32 + 2 * pair + 4 * direct}, [&] {
+    return cache.get(Key{M, N, stages, f32 + 2 * direct + 4 * (int)kind}, [&] {
         DensePlan best{kTileS, 1};
         double best_us = 0.0;
-        const double d = 1e-3 * stages * (f32 ? 32 : 64), sums = (double)M * N * (pair ? 2 : 1);
-        for (int t = 0; t < (f32 || !direct ? 2 : 4); ++t) {
-            const DenseModel& m = pair && t == kTileS ? (f32 ? kPairF32 : kPairBf16) : (f32 ? kDenseF32 : kDenseBf16)[t];
-            const long long cols = pair ? m.bn / 2 : m.bn, tiles = ((M + m.bm - 1ll) / m.bm) * ((N + cols - 1) / cols), padded = (tiles + kXcds - 1) / kXcds * kXcds;
+        const bool pair = kind == kDensePair;
+        const double k = 1e-3 * stages * (f32 ? 32 : 64), sums = 1e-6 * M * N * (pair ? 2 : 1);
+        for (const DenseModel& m : kDenseModels) {
+            if (m.kind != (int)kind || m.f32 != f32 || m.direct != direct) continue;
+            static const int kRows[] = {64, 128, 256, 256}, kCols[] = {64, 128, 128, 256}, kPairCols[] = {64, 64, 64, 128};
+            const long long bm = kRows[m.tile], bn = (pair ? kPairCols : kCols)[m.tile];
+            const long long tiles = ((M + bm - 1) / bm) * ((N + bn - 1) / bn), padded = (tiles + kXcds - 1) / kXcds * kXcds;
             for (int parts = 1; parts <= 16; ++parts) {
-                if (parts > 1 && (parts * 2 > stages || padded * parts > m.slots)) break;   // two stages to a part; parts side by side
-                const double groups = (double)(parts > 1 ? padded * parts : tiles);
-                const double us = m.fixed + std::ceil(groups / m.slots) * (m.round + (groups <= 256 ? m.alone : 1.0f) * m.per_k * d / parts) +
-                                  (parts > 1 ? kJoinUs + kPartUs * parts * sums : 0.0);
-                if (best_us == 0.0 || us < best_us) best = {t, parts}, best_us = us;
+                if (parts > 1 && (parts * 2 > stages || tiles * parts > (direct ? 560 : 1200))) break;   // two stages to a part, parts side by side
+                const double groups = (double)(parts > 1 ? padded * parts : tiles), rounds = std::ceil(groups / m.slots);
+                const double us = m.us[0] + rounds * (m.us[1] + m.us[2] * k / parts) + groups / m.slots * m.us[3] * k / parts + m.us[4] * sums +
+                                  (parts > 1 ? m.us[5] + m.us[6] * parts * sums : 0.0);
+                if (best_us == 0.0 || us < best_us) best = {m.tile, parts}, best_us = us;
             }
         }
         return best;
@@ -171,7 +216,7 @@ __global__ __launch_bounds__(256) void k_bias_rows(const float* __restrict__ bia
 }
 
 static DensePlan plan_forward(int B, int d_in, int n, bool f32, bool pair) {
-    return plan_dense(B, n, f32 ? stages_of<float>(d_in) : stages_of<uint16_t>(d_in), f32, pair, d_in % (f32 ? 4 : 8) == 0);
+    return plan_dense(pair ? kDensePair : kDenseForward, B, n, f32 ? stages_of<float>(d_in) : stages_of<uint16_t>(d_in), f32, d_in % (f32 ? 4 : 8) == 0);
 }
 
 template <typename T, typename TY>

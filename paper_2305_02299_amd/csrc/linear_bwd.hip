@@ -204,8 +204,8 @@ static BwdPlan plan_bwd(int B, int d_in, long long cols, long long K, long long 
     p.dz_bytes = whole((size_t)B * cols * elem);
     p.sum_bytes = whole((size_t)p.chunks * sum_cols * sizeof(float));
     const auto stages = [&](long long K) { return f32 ? stages_of<float>(K) : stages_of<uint16_t>(K); };
-    p.dx = plan_dense(B, d_in, stages(K), f32, false, direct);
-    p.dW = plan_dense((int)dW_rows, d_in, stages(B), f32, false, direct);
+    p.dx = plan_dense(kDenseGradX, B, d_in, stages(K), f32, direct);
+    p.dW = plan_dense(kDenseGradW, (int)dW_rows, d_in, stages(B), f32, direct);
     p.bytes = p.dz_bytes + p.sum_bytes + whole(std::max(part_bytes(p.dx, B, d_in, false), part_bytes(p.dW, (int)dW_rows, d_in, false)));
     return p;
 }
