@@ -14,6 +14,7 @@
 #pragma once
 #include "mma_tile.h"
 #include <initializer_list>
+#include <type_traits>
 
 namespace srigl {
 
@@ -160,10 +161,10 @@ __device__ __forceinline__ uint4 load_piece(const T* p, int valid) {
 }
 
 // Slot of piece q of line k, lines across K of R columns.  bf16: a read takes four lines (k % 4 = 0 .. 3) and 64 bytes of each: the 64-byte quarters of
-// 256 bytes are exchanged by the line; of 128-byte lines two share 256 bytes.  fp32: lines k and k + 4, 128 bytes of each.
+// 256 bytes are exchanged by the line; of 128-byte lines two share 256 bytes.  fp32: lines k and k + 8, 128 bytes of each.
 template <typename T, int R>
 __device__ __forceinline__ int across_swizzle(int k) {
-    if constexpr (sizeof(T) == 4) return ((k >> 2) & 1) << 3;
+    if constexpr (sizeof(T) == 4) return ((k >> 3) & 1) << 3;
     else return R >= 128 ? (k & 3) << 2 : ((k >> 1) & 1) << 2;
 }
 
@@ -188,7 +189,7 @@ struct FragReader {
             for (int b = 0; b < TB; ++b) {
                 if constexpr (sizeof(T) == 4) {
                     const int c = (first + b) * 32 + r;
-                    at[b] = 4 * half * PITCH + ((((c >> 2) ^ across_swizzle<T, R>(4 * half)) << 4) | ((c & 3) << 2));
+                    at[b] = 4 * half * PITCH + (c >> 2 << 4 | (c & 3) << 2);   // (steps of 8 lines by turns: the swizzle flips bit 7)
                 } else {
                     const int i = lane & 15, c = (first + b) * 32 + (lane & 16) + 4 * (i & 3);
                     at[b] = (8 * half + (i >> 2)) * PITCH + ((((c >> 3) ^ across_swizzle<T, R>(i >> 2)) << 4) | ((c & 4) << 1));
@@ -202,7 +203,7 @@ struct FragReader {
         } else if constexpr (sizeof(T) == 4) {
             F f;
 #pragma unroll
-            for (int j = 0; j < 4; ++j) f[j] = *reinterpret_cast<const float*>(stage + at[b] + (8 * kk + j) * PITCH);
+            for (int j = 0; j < 4; ++j) f[j] = *reinterpret_cast<const float*>(stage + (at[b] ^ (kk & 1 ? 128u : 0u)) + (8 * kk + j) * PITCH);
             return f;
         } else {
             union { s16x4_t part[2]; F f; } u;
@@ -213,6 +214,56 @@ struct FragReader {
         }
     }
 };
+
+// ---- fp32 on the bf16 units ----
+// An fp32 value is exactly the sum of three bf16 values, its upper, middle and lower eight bits (cut off, not rounded).  Of the nine products of two values the six that reach 2^-16 of the first go through
+// the bf16 units into the same fp32 sums; what is left out is below 2^-23 of the product (2^-25 on average), and sixteen products meet in one rounding where the fp32 instructions round every two.  Six
+// instructions of 32 clocks do what the fp32 ones do in 512 (2.7 times as fast); the lanes cut the values on their way from the LDS, 5.5 instructions a value, between the multiplications.  (Middle and lower
+// bits below 2^-126 count as zero: a value below 2^-110 loses its last bits, as far as its products matter beside others'.)  Infinities and NaN come out as NaN, and so does a sum that
+// leaves the range on its way: a tile with a sum that is not finite is computed again by the fp32 instructions.
+template <bool ALONG, int R, int TB>
+struct SplitReader {
+    static constexpr int PITCH = R * 4;
+    uint32_t at[ALONG ? 4 : TB];
+    __device__ __forceinline__ void init(int first, int lane) {
+        const int half = lane >> 5, r = lane & 31;
+        if constexpr (ALONG) {
+#pragma unroll
+            for (int q = 0; q < 4; ++q) at[q] = (first * 32 + r) * kLineBytes + (((4 * (q >> 1) + 2 * half + (q & 1)) ^ ((r >> 1) & 7)) << 4);
+        } else {
+#pragma unroll
+            for (int b = 0; b < TB; ++b) {
+                const int c = (first + b) * 32 + r;
+                at[b] = 8 * half * PITCH + ((((c >> 2) ^ across_swizzle<float, R>(8 * half)) << 4) | ((c & 3) << 2));
+            }
+        }
+    }
+    __device__ __forceinline__ void read(const unsigned char* stage, int b, int kk, f32x4_t (&v)[2]) const {
+#pragma unroll
+        for (int p = 0; p < 2; ++p)
+            if constexpr (ALONG) v[p] = *reinterpret_cast<const f32x4_t*>(stage + at[2 * kk + p] + b * 32 * kLineBytes);
+            else
+#pragma unroll
+                for (int j = 0; j < 4; ++j) v[p][j] = *reinterpret_cast<const float*>(stage + at[b] + (16 * kk + 4 * p + j) * PITCH);
+    }
+};
+struct SplitFrag { uint32_t part[3][4]; };
+// values 2 i and 2 i + 1 of a fragment
+__device__ __forceinline__ void split_pair(SplitFrag& f, const f32x4_t (&v)[2], int i) {
+    float x = v[i >> 1][2 * (i & 1)], y = v[i >> 1][2 * (i & 1) + 1];
+#pragma unroll
+    for (int p = 0; p < 3; ++p) {
+        f.part[p][i] = __builtin_amdgcn_perm(__float_as_uint(y), __float_as_uint(x), 0x07060302u);   // the upper halves of both
+        if (p < 2) {
+            x -= __uint_as_float(__float_as_uint(x) & 0xffff0000u);
+            y -= __uint_as_float(__float_as_uint(y) & 0xffff0000u);
+        }
+    }
+}
+__device__ __forceinline__ bf16x8_t split_part(const SplitFrag& f, int p) { return __builtin_bit_cast(bf16x8_t, *reinterpret_cast<const uint4*>(f.part[p])); }
+
+// The products in the order of their size, as parts of both values
+constexpr int kSplitA[6] = {2, 0, 1, 1, 0, 0}, kSplitB[6] = {0, 2, 1, 0, 1, 0};
 
 // ---- the product of a tile, staged through registers: any address, any size ----
 template <typename T, int R, int NT, class Op>
@@ -248,15 +299,15 @@ struct RegStage {
     }
 };
 
-// Stages h0 .. h1 - 1, whatever part of them there is
-template <typename T, int BM, int BN, int WGM, int WGN, class OA, class OB>
+// Stages h0 .. h1 - 1, whatever part of them there is.  SPLIT: fp32 on the bf16 units.
+template <typename T, bool SPLIT, int BM, int BN, int WGM, int WGN, class OA, class OB>
 __device__ __forceinline__ void product_of_tile(unsigned char* smem, const OA& oa, const OB& ob, int h0, int h1, f32x16_t (&acc)[BM / WGM / 32][BN / WGN / 32]) {
     constexpr int NT = WGM * WGN * 64, TM = BM / WGM / 32, TN = BN / WGN / 32, KSTEPS = kLineBytes / 32;
     const int lane = threadIdx.x & 63, wv = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), wm = wv / WGN, wn = wv % WGN;
     unsigned char *const sa = smem, *const sb = smem + BM * kLineBytes;
     if (h0 >= h1) return;
-    FragReader<T, OA::kAlong, BM, TM> fa;
-    FragReader<T, OB::kAlong, BN, TN> fb;
+    typename std::conditional<SPLIT, SplitReader<OA::kAlong, BM, TM>, FragReader<T, OA::kAlong, BM, TM>>::type fa;
+    typename std::conditional<SPLIT, SplitReader<OB::kAlong, BN, TN>, FragReader<T, OB::kAlong, BN, TN>>::type fb;
     fa.init(wm * TM, lane);
     fb.init(wn * TN, lane);
     RegStage<T, BM, NT, OA> ra;
@@ -272,6 +323,25 @@ __device__ __forceinline__ void product_of_tile(unsigned char* smem, const OA& o
             ra.load(oa, h + 1);
             rb.load(ob, h + 1);
         }
+        if constexpr (SPLIT) {
+#pragma unroll
+            for (int kk = 0; kk < KSTEPS / 2; ++kk) {
+                f32x4_t raw[TM + TN][2];
+                SplitFrag f[TM + TN];
+#pragma unroll
+                for (int i = 0; i < TM; ++i) fa.read(sa, i, kk, raw[i]);
+#pragma unroll
+                for (int j = 0; j < TN; ++j) fb.read(sb, j, kk, raw[TM + j]);
+#pragma unroll
+                for (int i = 0; i < 4 * (TM + TN); ++i) split_pair(f[i >> 2], raw[i >> 2], i & 3);
+#pragma unroll
+                for (int m = 0; m < 6 * TM * TN; ++m) {
+                    const int q = m % (TM * TN), p = m / (TM * TN);
+                    acc[q / TN][q % TN] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(split_part(f[q / TN], kSplitA[p]), split_part(f[TM + q % TN], kSplitB[p]), acc[q / TN][q % TN], 0, 0, 0);
+                }
+            }
+            continue;
+        } else {
 #pragma unroll
         for (int kk = 0; kk < KSTEPS; ++kk) {
             typename DenseFrag<T>::type a[TM], b[TN];
@@ -283,6 +353,7 @@ __device__ __forceinline__ void product_of_tile(unsigned char* smem, const OA& o
             for (int i = 0; i < TM; ++i)
 #pragma unroll
                 for (int j = 0; j < TN; ++j) dense_mma(acc[i][j], a[i], b[j]);
+        }
         }
     }
     __syncthreads();
@@ -392,6 +463,86 @@ __device__ __forceinline__ void direct_product_of_tile(unsigned char* smem, cons
                     for (int p = EARLY + m * (PASSES - EARLY) / N_MMA; p < EARLY + (m + 1) * (PASSES - EARLY) / N_MMA; ++p) issue_piece(p, h + NS - 1, before);
                 }
                 if (N_MMA == 1) dense_mma(acc[0][0], a[kk & 1][0], b[kk & 1][0]);   // (it waits for the one before: requests first)
+                __builtin_amdgcn_sched_barrier(0);
+            }
+        }
+        before = slot;
+        slot = after;
+    }
+    __builtin_amdgcn_s_waitcnt(vmcnt_imm(0));   // the stages requested again may still be landing in the ring
+    __syncthreads();
+}
+
+// Whole stages h0 .. h1 - 1 of an fp32 product by direct loads, as in direct_product_of_tile: two steps of 16 k a stage
+template <int BM, int BN, int WGM, int WGN, int NS, class OA, class OB>
+__device__ __forceinline__ void split_product_of_tile(unsigned char* smem, const OA& oa, const OB& ob, int h0, int h1, f32x16_t (&acc)[BM / WGM / 32][BN / WGN / 32]) {
+    constexpr int NWAVES = WGM * WGN, TM = BM / WGM / 32, TN = BN / WGN / 32, KSTEPS = 2, STAGE = (BM + BN) * kLineBytes;
+    using SA = DirectStage<float, BM, 0, NWAVES, OA>;
+    using SB = DirectStage<float, BN, BM * kLineBytes, NWAVES, OB>;
+    constexpr int PASSES = SA::PASSES + SB::PASSES, EARLY = PASSES / 2;
+    constexpr int N_FRAG = TM + TN, N_BLOCK = TM * TN, N_MMA = 6 * N_BLOCK, N_PAIR = 4 * N_FRAG, WAIT = N_MMA / 4 + 1;   // the cutting begins behind so many multiplications
+    static_assert(NS >= 2 && (NS - 1) * PASSES <= 63, "vmcnt range");
+    const int lane = threadIdx.x & 63, wv = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), wm = wv / WGN, wn = wv % WGN, n_st = h1 - h0;
+    if (n_st <= 0) return;
+    SA la;
+    SB lb;
+    la.init(oa, wv, lane);
+    lb.init(ob, wv, lane);
+    auto issue_piece = [&](int p, int h_unclamped, int slot) {
+        const int h = ob.index(h0 + min(h_unclamped, n_st - 1));
+        if (p < SA::PASSES) la.issue(oa, p, h, smem + slot, wv);
+        else lb.issue(ob, p - SA::PASSES, h, smem + slot, wv);
+    };
+#pragma unroll
+    for (int s = 0; s < NS; ++s)
+#pragma unroll
+        for (int p = 0; p < (s < NS - 1 ? PASSES : EARLY); ++p) issue_piece(p, s, s * STAGE);
+    SplitReader<OA::kAlong, BM, TM> fa;
+    SplitReader<OB::kAlong, BN, TN> fb;
+    fa.init(wm * TM, lane);
+    fb.init(wn * TN, lane);
+    f32x4_t raw[N_FRAG][2];
+    SplitFrag frag[2][N_FRAG];   // the TM of A, then the TN of B
+    auto read_raw = [&](int f, int slot, int kk) {
+        if (f < TM) fa.read(smem + slot, f, kk, raw[f]);
+        else fb.read(smem + slot + BM * kLineBytes, f - TM, kk, raw[f]);
+    };
+    __builtin_amdgcn_s_waitcnt(vmcnt_imm((NS - 2) * PASSES + EARLY));
+    __syncthreads();
+#pragma unroll
+    for (int f = 0; f < N_FRAG; ++f) read_raw(f, 0, 0);
+#pragma unroll
+    for (int i = 0; i < N_PAIR; ++i) split_pair(frag[0][i >> 2], raw[i >> 2], i & 3);
+    int slot = 0, before = (NS - 1) * STAGE;   // of stage h and of the one before it
+    for (int h = 0; h < n_st; ++h) {
+        const int after = slot == (NS - 1) * STAGE ? 0 : slot + STAGE;
+#pragma unroll
+        for (int kk = 0; kk < KSTEPS; ++kk) {
+            const bool last = kk + 1 == KSTEPS;
+            if (last) {   // this stage has been read; the next one must have landed
+                __builtin_amdgcn_s_waitcnt(kLgkm0);
+                __builtin_amdgcn_s_waitcnt(vmcnt_imm((NS - 2) * PASSES));
+                asm volatile("" ::: "memory");
+                __builtin_amdgcn_s_barrier();
+                asm volatile("" ::: "memory");
+            }
+#pragma unroll
+            for (int m = 0; m < N_MMA; ++m) {
+#pragma unroll
+                for (int f = m * N_FRAG / 2; f < (m + 1) * N_FRAG / 2 && f < N_FRAG; ++f) read_raw(f, last ? after : slot, last ? 0 : 1);
+                const int b = m % N_BLOCK, p = m / N_BLOCK;
+                acc[b / TN][b % TN] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(split_part(frag[kk][b / TN], kSplitA[p]), split_part(frag[kk][TM + b % TN], kSplitB[p]), acc[b / TN][b % TN], 0, 0, 0);
+                if (last) {
+#pragma unroll
+                    for (int q = m * EARLY / N_MMA; q < (m + 1) * EARLY / N_MMA; ++q) issue_piece(q, h + NS, slot);
+                } else {
+#pragma unroll
+                    for (int q = EARLY + m * (PASSES - EARLY) / N_MMA; q < EARLY + (m + 1) * (PASSES - EARLY) / N_MMA; ++q) issue_piece(q, h + NS - 1, before);
+                }
+                if (m >= WAIT) {
+#pragma unroll
+                    for (int i = (m - WAIT) * N_PAIR / (N_MMA - WAIT); i < (m + 1 - WAIT) * N_PAIR / (N_MMA - WAIT); ++i) split_pair(frag[kk ^ 1][i >> 2], raw[i >> 2], i & 3);
+                }
                 __builtin_amdgcn_sched_barrier(0);
             }
         }
@@ -664,6 +815,26 @@ __global__ __launch_bounds__(256) void k_dense_join(const float* __restrict__ pa
     }
 }
 
+// Whether some sum of the tile is not finite, for all wavefronts alike
+template <int NWAVES, int TM, int TN>
+__device__ __forceinline__ bool not_finite(unsigned char* smem, const f32x16_t (&acc)[TM][TN]) {
+    bool odd = false;
+#pragma unroll
+    for (int i = 0; i < TM; ++i)
+#pragma unroll
+        for (int j = 0; j < TN; ++j)
+#pragma unroll
+            for (int e = 0; e < 16; ++e) odd |= !(fabsf(acc[i][j][e]) <= 3.4028234e38f);
+    int* const flags = reinterpret_cast<int*>(smem);
+    const int any = __any(odd);
+    if ((threadIdx.x & 63) == 0) flags[threadIdx.x >> 6] = any;
+    __syncthreads();
+    odd = false;
+    for (int w = 0; w < NWAVES; ++w) odd |= flags[w] != 0;
+    __syncthreads();
+    return odd;
+}
+
 // M x N results (PAIR: of both products) of `stages` stages of K, in `parts` parts that are summed from `part` by a second launch.
 // NS: stages of the ring of direct loads, 0: staged through registers.
 template <typename T, int BM, int BN, int WGM, int WGN, int NS, bool PAIR, class OA, class OB, class Out>
@@ -684,13 +855,25 @@ __global__ __launch_bounds__(WGM * WGN * 64) void k_dense(OA oa, OB ob, int M, i
         for (int j = 0; j < BN / WGN / 32; ++j)
 #pragma unroll
             for (int e = 0; e < 16; ++e) acc[i][j][e] = 0.0f;
-    if constexpr (NS > 0) {
-        direct_product_of_tile<T, BM, BN, WGM, WGN, NS>(smem, oa, ob, h0, h1, acc);
-        if ((int)blockIdx.y == parts - 1)
-            for (int t = 0; t < ob.tails(); ++t) product_of_tile<T, BM, BN, WGM, WGN>(smem, oa, ob, ob.tail(t), ob.tail(t) + 1, acc);
-    } else {
-        product_of_tile<T, BM, BN, WGM, WGN>(smem, oa, ob, h0, h1, acc);
-    }
+    constexpr bool SPLIT = sizeof(T) == 4;
+    if constexpr (NS == 0) product_of_tile<T, SPLIT, BM, BN, WGM, WGN>(smem, oa, ob, h0, h1, acc);
+    else if constexpr (SPLIT) split_product_of_tile<BM, BN, WGM, WGN, NS>(smem, oa, ob, h0, h1, acc);
+    else direct_product_of_tile<T, BM, BN, WGM, WGN, NS>(smem, oa, ob, h0, h1, acc);
+    if constexpr (SPLIT)
+        if (not_finite<WGM * WGN>(smem, acc)) {
+#pragma unroll
+            for (int i = 0; i < BM / WGM / 32; ++i)
+#pragma unroll
+                for (int j = 0; j < BN / WGN / 32; ++j)
+#pragma unroll
+                    for (int e = 0; e < 16; ++e) acc[i][j][e] = 0.0f;
+            for (int h = h0; h < h1; ++h) {
+                const int stage = NS > 0 ? ob.index(h) : h;
+                product_of_tile<T, false, BM, BN, WGM, WGN>(smem, oa, ob, stage, stage + 1, acc);
+            }
+        }
+    if (NS > 0 && (int)blockIdx.y == parts - 1)
+        for (int t = 0; t < ob.tails(); ++t) product_of_tile<T, false, BM, BN, WGM, WGN>(smem, oa, ob, ob.tail(t), ob.tail(t) + 1, acc);
     if (parts > 1) {
         const long long pitch = PAIR ? 2ll * N : N;
         PartOut to{part + (size_t)blockIdx.y * M * pitch, N, pitch};
@@ -731,7 +914,7 @@ static srigl_status launch_tiles(const OA& oa, const OB& ob, int M, int N, int s
 
 // Tile and parts of K of a product (of a pair: N neurons, two sums each)
 struct DensePlan { int tile, parts; };
-enum { kTileS = 0, kTileM = 1, kTileH = 2, kTileL = 3 };   // 64 x 64 (of a pair 64 x 128), 128 x 128, 256 x 128 and 256 x 256 (bf16, direct loads)
+enum { kTileS = 0, kTileM = 1, kTileH = 2, kTileL = 3 };   // 64 x 64 (of a pair 64 x 128), 128 x 128, 256 x 128 (direct loads) and 256 x 256 (and bf16)
 enum DenseKind { kDenseForward = 0, kDensePair = 1, kDenseGradX = 2, kDenseGradW = 3 };   // a layer's forward product, a gated block's, gradients of x and of W
 // direct: rows are multiples of 16 bytes (a choice by sizes, so that the workspace does not depend on addresses)
 DensePlan plan_dense(DenseKind kind, int M, int N, int stages, bool f32, bool direct);
@@ -746,14 +929,13 @@ static srigl_status launch_dense(const OA& oa, const OB& ob, int M, int N, int s
         if (plan.tile == kTileS) return launch_tiles<T, 64, SN, 2, 2, 0, PAIR>(oa, ob, M, N, stages, plan.parts, out, part, st);
         return launch_tiles<T, 128, 128, 2, 2, 0, PAIR>(oa, ob, M, N, stages, plan.parts, out, part, st);
     }
-    if constexpr (sizeof(T) == 2) {
+    if constexpr (sizeof(T) == 2)
         if (plan.tile == kTileL) return launch_tiles<T, 256, 256, 2, 4, 2, PAIR>(oa, ob, M, N, stages, plan.parts, out, part, st);
-        if (plan.tile == kTileH) return launch_tiles<T, 256, 128, 4, 2, 3, PAIR>(oa, ob, M, N, stages, plan.parts, out, part, st);
-    }
-    // 128 x 128 by eight wavefronts (four of 64 x 64 leave each SIMD one, which waits at every barrier: bf16 512 rows, 768 -> 3072, 15.2 us, now 11.5; fp32 2048 rows, 4096 -> 4096, 513 and 496), in bf16
-    // only where both operands' lines run along K: the transposing reads of half as wide wavefronts are 1.5 times as many (gradient of W, 2048 rows, 4096 -> 4096, 83.5 us against 77.8)
-    constexpr bool EIGHT = sizeof(T) == 4 || (OA::kAlong && OB::kAlong);
-    if (plan.tile != kTileS) return launch_tiles<T, 128, 128, EIGHT && PAIR ? 4 : 2, EIGHT && !PAIR ? 4 : 2, 4, PAIR>(oa, ob, M, N, stages, plan.parts, out, part, st);
+    if (plan.tile >= kTileH) return launch_tiles<T, 256, 128, 4, 2, 3, PAIR>(oa, ob, M, N, stages, plan.parts, out, part, st);
+    // 128 x 128 by eight wavefronts where both operands' lines run along K, in bf16 (four of 64 x 64 leave each SIMD one, which waits at every barrier: 512 rows, 768 -> 3072, 15.2 us, now 11.5); the
+    // transposing reads of half as wide wavefronts are 1.5 times as many (gradient of W, 2048 rows, 4096 -> 4096, 83.5 us against 77.8), and so is the cutting of fp32 (forward, 409 and 364)
+    constexpr bool EIGHT = sizeof(T) == 2 && OA::kAlong && OB::kAlong;
+    if (plan.tile == kTileM) return launch_tiles<T, 128, 128, EIGHT && PAIR ? 4 : 2, EIGHT && !PAIR ? 4 : 2, 4, PAIR>(oa, ob, M, N, stages, plan.parts, out, part, st);
     return launch_tiles<T, 64, SN, 2, 2, 4, PAIR>(oa, ob, M, N, stages, plan.parts, out, part, st);
 }
 // ---- few rows of x ----
