@@ -783,38 +783,6 @@ struct PartOut {
         store_values<float, V>(part + (size_t)m * pitch + N + c, w, valid);
     }
 };
-// (eight parts' values are requested together: a thread waits for memory once or twice)
-template <class Out, int V, bool PAIR>
-__global__ __launch_bounds__(256) void k_dense_join(const float* __restrict__ part, int parts, int M, int N, Out out) {
-    constexpr int TOGETHER = 8;
-    const int c = (blockIdx.x * 256 + threadIdx.x) * V, valid = N - c;
-    if (valid <= 0) return;
-    out.template start<V>(c, valid);
-    const long long pitch = PAIR ? 2ll * N : N;
-    for (int m = blockIdx.y; m < M; m += gridDim.y) {
-        float v[V] = {}, w[V] = {};
-        for (int z0 = 0; z0 < parts; z0 += TOGETHER) {
-            float t[TOGETHER][V] = {}, u[TOGETHER][V] = {};
-#pragma unroll
-            for (int k = 0; k < TOGETHER; ++k) {
-                const float* const p = part + ((size_t)min(z0 + k, parts - 1) * M + m) * pitch + c;
-                load_values<float, V>(p, t[k], valid);
-                if constexpr (PAIR) load_values<float, V>(p + N, u[k], valid);
-            }
-#pragma unroll
-            for (int k = 0; k < TOGETHER; ++k)
-                if (z0 + k < parts)
-#pragma unroll
-                    for (int q = 0; q < V; ++q) {
-                        v[q] += t[k][q];
-                        if constexpr (PAIR) w[q] += u[k][q];
-                    }
-        }
-        if constexpr (PAIR) out.template row<V>(m, c, valid, v, w);
-        else out.template row<V>(m, c, valid, v);
-    }
-}
-
 // Whether some sum of the tile is not finite, for all wavefronts alike
 template <int NWAVES, int TM, int TN>
 __device__ __forceinline__ bool not_finite(unsigned char* smem, const f32x16_t (&acc)[TM][TN]) {
@@ -835,80 +803,168 @@ __device__ __forceinline__ bool not_finite(unsigned char* smem, const f32x16_t (
     return odd;
 }
 
-// M x N results (PAIR: of both products) of `stages` stages of K, in `parts` parts that are summed from `part` by a second launch.
-// NS: stages of the ring of direct loads, 0: staged through registers.
+// One product: M x N results (PAIR: of both matrices) of `stages` stages of K, in `parts` parts whose sums go to `part` and are joined by a second launch.
+template <class OA, class OB, class Out>
+struct DenseProduct {
+    OA oa;
+    OB ob;
+    Out out;
+    int M, N, stages, parts;
+    float* part;
+};
+
+// Tile `id` (of tile_of_workgroup's order) and part `part_no` of a product.  NS: stages of the ring of direct loads, 0: staged through registers.
 template <typename T, int BM, int BN, int WGM, int WGN, int NS, bool PAIR, class OA, class OB, class Out>
-__global__ __launch_bounds__(WGM * WGN * 64) void k_dense(OA oa, OB ob, int M, int N, int stages, int parts, Out out, float* part) {
-    extern __shared__ __attribute__((aligned(1024))) unsigned char smem[];
+__device__ __forceinline__ void dense_tile(unsigned char* smem, int id, int part_no, DenseProduct<OA, OB, Out>& p) {
     constexpr int COLS = PAIR ? BN / 2 : BN, V = kPiece<T>;
     int tile_m, tile_n;
-    if (!tile_of_workgroup(blockIdx.x, (M + BM - 1) / BM, (N + COLS - 1) / COLS, &tile_m, &tile_n)) return;
-    const int m0 = tile_m * BM, n0 = tile_n * COLS;
-    oa.move(m0);
-    ob.move(n0);
-    if (NS > 0) stages = ob.whole();
-    const int h0 = parts == 1 ? 0 : (int)((long long)blockIdx.y * stages / parts), h1 = parts == 1 ? stages : (int)((long long)(blockIdx.y + 1) * stages / parts);
+    if (!tile_of_workgroup(id, (p.M + BM - 1) / BM, (p.N + COLS - 1) / COLS, &tile_m, &tile_n)) return;
+    const int m0 = tile_m * BM, n0 = tile_n * COLS, parts = p.parts;
+    p.oa.move(m0);
+    p.ob.move(n0);
+    const int stages = NS > 0 ? p.ob.whole() : p.stages;
+    const int h0 = parts == 1 ? 0 : (int)((long long)part_no * stages / parts), h1 = parts == 1 ? stages : (int)((long long)(part_no + 1) * stages / parts);
     f32x16_t acc[BM / WGM / 32][BN / WGN / 32];
+    const auto clear = [&] {
 #pragma unroll
-    for (int i = 0; i < BM / WGM / 32; ++i)
+        for (int i = 0; i < BM / WGM / 32; ++i)
 #pragma unroll
-        for (int j = 0; j < BN / WGN / 32; ++j)
+            for (int j = 0; j < BN / WGN / 32; ++j)
 #pragma unroll
-            for (int e = 0; e < 16; ++e) acc[i][j][e] = 0.0f;
+                for (int e = 0; e < 16; ++e) acc[i][j][e] = 0.0f;
+    };
+    clear();
     constexpr bool SPLIT = sizeof(T) == 4;
-    if constexpr (NS == 0) product_of_tile<T, SPLIT, BM, BN, WGM, WGN>(smem, oa, ob, h0, h1, acc);
-    else if constexpr (SPLIT) split_product_of_tile<BM, BN, WGM, WGN, NS>(smem, oa, ob, h0, h1, acc);
-    else direct_product_of_tile<T, BM, BN, WGM, WGN, NS>(smem, oa, ob, h0, h1, acc);
+    if constexpr (NS == 0) product_of_tile<T, SPLIT, BM, BN, WGM, WGN>(smem, p.oa, p.ob, h0, h1, acc);
+    else if constexpr (SPLIT) split_product_of_tile<BM, BN, WGM, WGN, NS>(smem, p.oa, p.ob, h0, h1, acc);
+    else direct_product_of_tile<T, BM, BN, WGM, WGN, NS>(smem, p.oa, p.ob, h0, h1, acc);
     if constexpr (SPLIT)
         if (not_finite<WGM * WGN>(smem, acc)) {
-#pragma unroll
-            for (int i = 0; i < BM / WGM / 32; ++i)
-#pragma unroll
-                for (int j = 0; j < BN / WGN / 32; ++j)
-#pragma unroll
-                    for (int e = 0; e < 16; ++e) acc[i][j][e] = 0.0f;
+            clear();
             for (int h = h0; h < h1; ++h) {
-                const int stage = NS > 0 ? ob.index(h) : h;
-                product_of_tile<T, false, BM, BN, WGM, WGN>(smem, oa, ob, stage, stage + 1, acc);
+                const int stage = NS > 0 ? p.ob.index(h) : h;
+                product_of_tile<T, false, BM, BN, WGM, WGN>(smem, p.oa, p.ob, stage, stage + 1, acc);
             }
         }
-    if (NS > 0 && (int)blockIdx.y == parts - 1)
-        for (int t = 0; t < ob.tails(); ++t) product_of_tile<T, false, BM, BN, WGM, WGN>(smem, oa, ob, ob.tail(t), ob.tail(t) + 1, acc);
+    if (NS > 0 && part_no == parts - 1)
+        for (int t = 0; t < p.ob.tails(); ++t) product_of_tile<T, false, BM, BN, WGM, WGN>(smem, p.oa, p.ob, p.ob.tail(t), p.ob.tail(t) + 1, acc);
     if (parts > 1) {
-        const long long pitch = PAIR ? 2ll * N : N;
-        PartOut to{part + (size_t)blockIdx.y * M * pitch, N, pitch};
-        if constexpr (PAIR) pair_as_rows<BM, BN, WGM, WGN, 4>(smem, acc, m0, n0, M, N, to);
-        else tile_as_rows<BM, BN, WGM, WGN, 4>(smem, acc, m0, n0, M, N, to);
+        const long long pitch = PAIR ? 2ll * p.N : p.N;
+        PartOut to{p.part + (size_t)part_no * p.M * pitch, p.N, pitch};
+        if constexpr (PAIR) pair_as_rows<BM, BN, WGM, WGN, 4>(smem, acc, m0, n0, p.M, p.N, to);
+        else tile_as_rows<BM, BN, WGM, WGN, 4>(smem, acc, m0, n0, p.M, p.N, to);
         return;
     }
     if constexpr (Out::kListed)
-        if (out.active) {
-            listed_as_rows<BM, BN, WGM, WGN, V>(smem, acc, m0, n0, M, out);
+        if (p.out.active) {
+            listed_as_rows<BM, BN, WGM, WGN, V>(smem, acc, m0, n0, p.M, p.out);
             return;
         }
-    if constexpr (PAIR) pair_as_rows<BM, BN, WGM, WGN, V>(smem, acc, m0, n0, M, N, out);
-    else tile_as_rows<BM, BN, WGM, WGN, V>(smem, acc, m0, n0, M, N, out);
+    if constexpr (PAIR) pair_as_rows<BM, BN, WGM, WGN, V>(smem, acc, m0, n0, p.M, p.N, p.out);
+    else tile_as_rows<BM, BN, WGM, WGN, V>(smem, acc, m0, n0, p.M, p.N, p.out);
+}
+
+template <typename T, int BM, int BN, int WGM, int WGN, int NS, bool PAIR, class P>
+__global__ __launch_bounds__(WGM * WGN * 64) void k_dense(P p) {
+    extern __shared__ __attribute__((aligned(1024))) unsigned char smem[];
+    dense_tile<T, BM, BN, WGM, WGN, NS, PAIR>(smem, blockIdx.x, blockIdx.y, p);
+}
+
+// Two products that do not wait for each other in one launch (the gradients of x and of W): what one leaves idle the other takes, and a small pass is a launch shorter.  The first one's workgroups come
+// first, then the second one's; both are whole multiples of 8 a part, so that a workgroup's die is the one that tile_of_workgroup expects.
+template <typename T, int BM, int BN, int WGM, int WGN, int NS, class P, class Q>
+__global__ __launch_bounds__(WGM * WGN * 64) void k_dense_two(P p, Q q, int p_wg, int q_wg) {
+    extern __shared__ __attribute__((aligned(1024))) unsigned char smem[];
+    int id = blockIdx.x;
+    if (id < p_wg * p.parts) {
+        dense_tile<T, BM, BN, WGM, WGN, NS, false>(smem, id % p_wg, id / p_wg, p);
+    } else {
+        id -= p_wg * p.parts;
+        dense_tile<T, BM, BN, WGM, WGN, NS, false>(smem, id % q_wg, id / q_wg, q);
+    }
+}
+
+// ---- joining the parts' sums: a thread takes V columns of a row; eight parts' values are requested together, so that it waits for memory once or twice ----
+template <int V, bool PAIR, class P>
+__device__ __forceinline__ void dense_join(long long item, P& p) {
+    constexpr int TOGETHER = 8;
+    const int groups = (p.N + V - 1) / V, m = (int)(item / groups), c = (int)(item - (long long)m * groups) * V, valid = p.N - c;
+    if (m >= p.M) return;
+    p.out.template start<V>(c, valid);
+    const long long pitch = PAIR ? 2ll * p.N : p.N;
+    float v[V] = {}, w[V] = {};
+    for (int z0 = 0; z0 < p.parts; z0 += TOGETHER) {
+        float t[TOGETHER][V] = {}, u[TOGETHER][V] = {};
+#pragma unroll
+        for (int k = 0; k < TOGETHER; ++k) {
+            const float* const at = p.part + ((size_t)min(z0 + k, p.parts - 1) * p.M + m) * pitch + c;
+            load_values<float, V>(at, t[k], valid);
+            if constexpr (PAIR) load_values<float, V>(at + p.N, u[k], valid);
+        }
+#pragma unroll
+        for (int k = 0; k < TOGETHER; ++k)
+            if (z0 + k < p.parts)
+#pragma unroll
+                for (int q = 0; q < V; ++q) {
+                    v[q] += t[k][q];
+                    if constexpr (PAIR) w[q] += u[k][q];
+                }
+    }
+    if constexpr (PAIR) p.out.template row<V>(m, c, valid, v, w);
+    else p.out.template row<V>(m, c, valid, v);
+}
+template <int V, bool PAIR, class P>
+__global__ __launch_bounds__(256) void k_dense_join(P p) { dense_join<V, PAIR>((long long)blockIdx.x * 256 + threadIdx.x, p); }
+template <class P, class Q>
+__global__ __launch_bounds__(256) void k_dense_join_two(P p, Q q, unsigned p_groups) {
+    if (blockIdx.x < p_groups) dense_join<4, false>((long long)blockIdx.x * 256 + threadIdx.x, p);
+    else dense_join<4, false>((long long)(blockIdx.x - p_groups) * 256 + threadIdx.x, q);
+}
+// workgroups of a join
+template <class P> inline long long join_groups(const P& p, int V) { return p.parts > 1 ? ((long long)p.M * ((p.N + V - 1ll) / V) + 255) / 256 : 0; }
+
+template <int BM, int BN, int WGM, int NS, bool LISTED>
+constexpr size_t dense_lds() {
+    const size_t ring = (size_t)(NS > 0 ? NS : 1) * (BM + BN) * kLineBytes, rows = LISTED ? EpiLayout<BN, WGM>::BYTES : rows_lds<BM, BN, WGM>();
+    return ring > rows ? ring : rows;
+}
+// workgroups of a part
+template <int BM, int COLS, class P> inline long long dense_groups(const P& p) {
+    return (((p.M + BM - 1ll) / BM) * ((p.N + COLS - 1ll) / COLS) + kXcds - 1) / kXcds * kXcds;
 }
 
 template <typename T, int BM, int BN, int WGM, int WGN, int NS, bool PAIR, class OA, class OB, class Out>
-static srigl_status launch_tiles(const OA& oa, const OB& ob, int M, int N, int stages, int parts, const Out& out, float* part, hipStream_t st) {
-    constexpr size_t ring = (size_t)std::max(NS, 1) * (BM + BN) * kLineBytes, rows = Out::kListed ? EpiLayout<BN, WGM>::BYTES : rows_lds<BM, BN, WGM>(), lds = ring > rows ? ring : rows;
+static srigl_status launch_tiles(const DenseProduct<OA, OB, Out>& p, hipStream_t st) {
+    using P = DenseProduct<OA, OB, Out>;
+    constexpr size_t lds = dense_lds<BM, BN, WGM, NS, Out::kListed>();
     static_assert(lds <= kLdsMax, "LDS");
-    constexpr int COLS = PAIR ? BN / 2 : BN;
-    auto kern = k_dense<T, BM, BN, WGM, WGN, NS, PAIR, OA, OB, Out>;
+    auto kern = k_dense<T, BM, BN, WGM, WGN, NS, PAIR, P>;
     static LdsLimit limit;
     if (limit.ensure(kern, lds) != SRIGL_OK) return SRIGL_ERR_HIP;
-    const long long tiles = ((M + BM - 1ll) / BM) * ((N + COLS - 1ll) / COLS), n_wg = (tiles + kXcds - 1) / kXcds * kXcds;
-    if (n_wg > 0x7fffffffll || parts < 1 || parts > 65535) return SRIGL_ERR_UNSUPPORTED;
-    hipLaunchKernelGGL(kern, dim3((unsigned)n_wg, (unsigned)parts), dim3(WGM * WGN * 64), lds, st, oa, ob, M, N, stages, parts, out, part);
-    if (parts > 1) {
+    const long long n_wg = dense_groups<BM, PAIR ? BN / 2 : BN>(p);
+    if (n_wg > 0x7fffffffll || p.parts < 1 || p.parts > 65535) return SRIGL_ERR_UNSUPPORTED;
+    hipLaunchKernelGGL(kern, dim3((unsigned)n_wg, (unsigned)p.parts), dim3(WGM * WGN * 64), lds, st, p);
+    if (p.parts > 1) {
         bool one = false;   // a neuron to a thread, which writes the ablated columns in front of its own too
-        if constexpr (Out::kListed) one = out.active != nullptr;
-        const dim3 grid((unsigned)(one ? (N + 255ll) / 256 : (N + 1023ll) / 1024), (unsigned)std::min(M, 65535));
-        if constexpr (Out::kListed)
-            if (one) hipLaunchKernelGGL((k_dense_join<Out, 1, PAIR>), grid, dim3(256), 0, st, part, parts, M, N, out);
-        if (!one) hipLaunchKernelGGL((k_dense_join<Out, 4, PAIR>), grid, dim3(256), 0, st, part, parts, M, N, out);
+        if constexpr (Out::kListed) {
+            one = p.out.active != nullptr;
+            if (one) hipLaunchKernelGGL((k_dense_join<1, PAIR, P>), dim3((unsigned)join_groups(p, 1)), dim3(256), 0, st, p);
+        }
+        if (!one) hipLaunchKernelGGL((k_dense_join<4, PAIR, P>), dim3((unsigned)join_groups(p, 4)), dim3(256), 0, st, p);
     }
+    return hip_ok(hipGetLastError());
+}
+template <typename T, int BM, int BN, int WGM, int WGN, int NS, class P, class Q>
+static srigl_status launch_tiles_two(const P& p, const Q& q, hipStream_t st) {
+    constexpr size_t lds = dense_lds<BM, BN, WGM, NS, false>();
+    auto kern = k_dense_two<T, BM, BN, WGM, WGN, NS, P, Q>;
+    static LdsLimit limit;
+    if (limit.ensure(kern, lds) != SRIGL_OK) return SRIGL_ERR_HIP;
+    const long long p_wg = dense_groups<BM, BN>(p), q_wg = dense_groups<BM, BN>(q), all = p_wg * p.parts + q_wg * q.parts;
+    if (all > 0x7fffffffll) return SRIGL_ERR_UNSUPPORTED;
+    hipLaunchKernelGGL(kern, dim3((unsigned)all), dim3(WGM * WGN * 64), lds, st, p, q, (int)p_wg, (int)q_wg);
+    const long long pj = join_groups(p, 4), qj = join_groups(q, 4);
+    if (pj + qj > 0) hipLaunchKernelGGL((k_dense_join_two<P, Q>), dim3((unsigned)(pj + qj)), dim3(256), 0, st, p, q, (unsigned)pj);
     return hip_ok(hipGetLastError());
 }
 
@@ -918,25 +974,41 @@ enum { kTileS = 0, kTileM = 1, kTileH = 2, kTileL = 3 };   // 64 x 64 (of a pair
 enum DenseKind { kDenseForward = 0, kDensePair = 1, kDenseGradX = 2, kDenseGradW = 3 };   // a layer's forward product, a gated block's, gradients of x and of W
 // direct: rows are multiples of 16 bytes (a choice by sizes, so that the workspace does not depend on addresses)
 DensePlan plan_dense(DenseKind kind, int M, int N, int stages, bool f32, bool direct);
+// Both gradients' products (of x: B x d_in over K; of W: rows x d_in over B): tile and parts of each; together: one launch in tiles of one shape
+struct DensePlans { DensePlan dx, dW; bool together; };
+DensePlans plan_gradients(int B, int d_in, int K_stages, int rows, int B_stages, bool f32, bool direct);
 // bytes of the parts' sums
 inline size_t part_bytes(DensePlan p, int M, int N, bool pair) { return p.parts > 1 ? (size_t)p.parts * M * N * (pair ? 2 : 1) * sizeof(float) : 0; }
 
 template <typename T, bool PAIR, class OA, class OB, class Out>
-static srigl_status launch_dense(const OA& oa, const OB& ob, int M, int N, int stages, DensePlan plan, const Out& out, float* part, hipStream_t st) {
-    if (M <= 0 || N <= 0) return SRIGL_OK;
+static srigl_status launch_dense(const DenseProduct<OA, OB, Out>& p, int tile, hipStream_t st) {
+    if (p.M <= 0 || p.N <= 0) return SRIGL_OK;
     constexpr int SN = PAIR ? 128 : 64;
-    if (!(oa.direct(256) && ob.direct(256))) {
-        if (plan.tile == kTileS) return launch_tiles<T, 64, SN, 2, 2, 0, PAIR>(oa, ob, M, N, stages, plan.parts, out, part, st);
-        return launch_tiles<T, 128, 128, 2, 2, 0, PAIR>(oa, ob, M, N, stages, plan.parts, out, part, st);
+    if (!(p.oa.direct(256) && p.ob.direct(256))) {
+        if (tile == kTileS) return launch_tiles<T, 64, SN, 2, 2, 0, PAIR>(p, st);
+        return launch_tiles<T, 128, 128, 2, 2, 0, PAIR>(p, st);
     }
     if constexpr (sizeof(T) == 2)
-        if (plan.tile == kTileL) return launch_tiles<T, 256, 256, 2, 4, 2, PAIR>(oa, ob, M, N, stages, plan.parts, out, part, st);
-    if (plan.tile >= kTileH) return launch_tiles<T, 256, 128, 4, 2, 3, PAIR>(oa, ob, M, N, stages, plan.parts, out, part, st);
+        if (tile == kTileL) return launch_tiles<T, 256, 256, 2, 4, 2, PAIR>(p, st);
+    if (tile >= kTileH) return launch_tiles<T, 256, 128, 4, 2, 3, PAIR>(p, st);
     // 128 x 128 by eight wavefronts where both operands' lines run along K, in bf16 (four of 64 x 64 leave each SIMD one, which waits at every barrier: 512 rows, 768 -> 3072, 15.2 us, now 11.5); the
     // transposing reads of half as wide wavefronts are 1.5 times as many (gradient of W, 2048 rows, 4096 -> 4096, 83.5 us against 77.8), and so is the cutting of fp32 (forward, 409 and 364)
     constexpr bool EIGHT = sizeof(T) == 2 && OA::kAlong && OB::kAlong;
-    if (plan.tile == kTileM) return launch_tiles<T, 128, 128, EIGHT && PAIR ? 4 : 2, EIGHT && !PAIR ? 4 : 2, 4, PAIR>(oa, ob, M, N, stages, plan.parts, out, part, st);
-    return launch_tiles<T, 64, SN, 2, 2, 4, PAIR>(oa, ob, M, N, stages, plan.parts, out, part, st);
+    if (tile == kTileM) return launch_tiles<T, 128, 128, EIGHT && PAIR ? 4 : 2, EIGHT && !PAIR ? 4 : 2, 4, PAIR>(p, st);
+    return launch_tiles<T, 64, SN, 2, 2, 4, PAIR>(p, st);
+}
+// Both products in tiles of one shape, side by side
+template <typename T, class P, class Q>
+static srigl_status launch_dense_two(const P& p, const Q& q, int tile, hipStream_t st) {
+    if (!(p.oa.direct(256) && p.ob.direct(256) && q.oa.direct(256) && q.ob.direct(256))) {
+        if (tile == kTileS) return launch_tiles_two<T, 64, 64, 2, 2, 0>(p, q, st);
+        return launch_tiles_two<T, 128, 128, 2, 2, 0>(p, q, st);
+    }
+    if constexpr (sizeof(T) == 2)
+        if (tile == kTileL) return launch_tiles_two<T, 256, 256, 2, 4, 2>(p, q, st);
+    if (tile >= kTileH) return launch_tiles_two<T, 256, 128, 4, 2, 3>(p, q, st);
+    if (tile == kTileM) return launch_tiles_two<T, 128, 128, 2, 2, 4>(p, q, st);
+    return launch_tiles_two<T, 64, 64, 2, 2, 4>(p, q, st);
 }
 // ---- few rows of x ----
 // Products with at most 64 rows of x are bound by reading the weights.  A workgroup takes 16 neurons (of a pair: of both matrices) and all of K, its wavefronts 128 bytes of the lines in turn, straight

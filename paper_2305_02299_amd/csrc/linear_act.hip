@@ -10,8 +10,8 @@ namespace srigl {
 
 // Expected time (us) of a product in a tile and `parts` parts of K: a fixed part, a part a round of workgroups over the compute units and, by 1000 elements of K, a part a round and one that follows how
 // full the rounds are, a part per million results, a second launch and the parts' sums (a million of them written and read) where there are several.  Non-negative least squares on the relative error of
-// 170000 timings in graphs, every tile and 1 to 16 parts of 29000 random products (17 to 2048 rows, 100 to 4096 wide, 100 to 16384 neurons): 3 to 12 % a timing; the tile and parts of smallest time are 0.1
-// to 1.1 % behind the fastest on average by kind and type, 8 % at worst in 95 of 100, 37 % at worst.
+// 180000 timings in graphs, every tile and 1 to 16 parts of 30000 random products (17 to 2048 rows, 100 to 4096 wide, 100 to 16384 neurons): 4 to 10 % a timing; the tile and parts of smallest time are 0.1
+// to 1.3 % behind the fastest on average by kind and type, 8 % at worst in 95 of 100, 37 % at worst.
 struct DenseModel {
     int kind, f32, direct, tile, slots;
     float us[7];   // fixed, round, per_k, per_k_full, results, second, part
@@ -23,63 +23,133 @@ static const DenseModel kDenseModels[] = {
     {0, 0, 1, 1, 256, {4.8f, 3.06f, 5.67f, 4.17f, 0.502f, 2.24f, 1.63f}},
     {0, 0, 1, 2, 256, {7.47f, 2.08f, 8.42f, 5.26f, 0.699f, 2.13f, 1.48f}},
     {0, 0, 1, 3, 256, {10.5f, 3.56f, 15.1f, 9.99f, 0.505f, 1.13f, 1.14f}},
-    {0, 1, 0, 0, 256, {5.67f, 0.0315f, 20.9f, 0.0f, 1.11f, 2.17f, 1.88f}},
-    {0, 1, 0, 1, 256, {10.2f, 0.0f, 66.2f, 2.89f, 0.684f, 0.902f, 1.5f}},
-    {0, 1, 1, 0, 256, {5.59f, 0.409f, 16.9f, 1.5f, 1.22f, 2.63f, 1.91f}},
-    {0, 1, 1, 1, 256, {6.32f, 2.1f, 56.7f, 7.6f, 0.948f, 3.35f, 1.7f}},
+    {0, 1, 0, 0, 512, {5.57f, 0.363f, 19.8f, 13.9f, 1.26f, 2.37f, 1.98f}},
+    {0, 1, 0, 1, 512, {10.9f, 0.0f, 49.0f, 32.5f, 0.884f, 0.751f, 1.53f}},
+    {0, 1, 1, 0, 256, {6.61f, 0.0f, 15.5f, 0.0f, 1.55f, 2.72f, 1.87f}},
+    {0, 1, 1, 1, 256, {8.27f, 4.51f, 31.1f, 10.7f, 1.28f, 1.27f, 1.61f}},
+    {0, 1, 1, 2, 256, {10.2f, 3.03f, 56.5f, 17.2f, 0.884f, 2.43f, 1.5f}},
     {1, 0, 0, 0, 1024, {7.51f, 0.0f, 9.0f, 21.7f, 0.416f, 2.47f, 1.7f}},
     {1, 0, 0, 1, 512, {10.4f, 0.0f, 12.5f, 10.0f, 0.361f, 2.25f, 1.3f}},
     {1, 0, 1, 0, 256, {3.6f, 3.77f, 4.39f, 2.74f, 0.488f, 2.62f, 1.53f}},
     {1, 0, 1, 1, 256, {4.13f, 3.35f, 5.59f, 4.26f, 0.343f, 2.83f, 1.63f}},
     {1, 0, 1, 2, 256, {6.5f, 2.58f, 8.5f, 4.94f, 0.55f, 2.73f, 1.46f}},
     {1, 0, 1, 3, 256, {9.16f, 3.71f, 15.3f, 9.14f, 0.348f, 2.44f, 1.12f}},
-    {1, 1, 0, 0, 256, {6.75f, 0.0f, 36.2f, 0.0f, 0.531f, 2.66f, 1.51f}},
-    {1, 1, 0, 1, 256, {8.73f, 0.0f, 65.8f, 0.0f, 0.653f, 2.51f, 1.38f}},
-    {1, 1, 1, 0, 256, {3.88f, 3.3f, 31.4f, 5.3f, 0.807f, 3.44f, 1.57f}},
-    {1, 1, 1, 1, 256, {5.21f, 2.3f, 57.0f, 6.95f, 0.709f, 4.32f, 1.76f}},
+    {1, 1, 0, 0, 768, {6.89f, 0.0f, 29.4f, 44.4f, 0.719f, 3.07f, 1.73f}},
+    {1, 1, 0, 1, 512, {9.19f, 0.0f, 48.5f, 36.9f, 0.664f, 2.69f, 1.42f}},
+    {1, 1, 1, 0, 256, {3.68f, 4.28f, 22.4f, 6.52f, 0.75f, 3.52f, 1.48f}},
+    {1, 1, 1, 1, 256, {6.43f, 4.67f, 31.6f, 10.7f, 0.962f, 3.2f, 1.54f}},
+    {1, 1, 1, 2, 256, {8.04f, 3.38f, 56.6f, 18.0f, 0.745f, 4.64f, 1.38f}},
     {2, 0, 0, 0, 1536, {5.67f, 0.0f, 11.0f, 13.7f, 0.375f, 2.93f, 2.48f}},
     {2, 0, 0, 1, 1536, {8.5f, 0.0f, 16.4f, 30.0f, 0.123f, 3.27f, 1.67f}},
     {2, 0, 1, 0, 256, {7.2f, 0.119f, 3.6f, 1.06f, 0.503f, 2.87f, 2.85f}},
     {2, 0, 1, 1, 256, {7.95f, 1.58f, 5.67f, 3.77f, 0.394f, 3.38f, 2.38f}},
     {2, 0, 1, 2, 256, {9.2f, 0.299f, 8.67f, 4.92f, 0.479f, 3.87f, 1.88f}},
     {2, 0, 1, 3, 256, {10.8f, 0.656f, 15.9f, 8.48f, 0.602f, 4.97f, 1.46f}},
-    {2, 1, 0, 0, 1536, {1.59f, 3.58f, 28.0f, 67.0f, 1.34f, 2.57f, 2.99f}},
-    {2, 1, 0, 1, 256, {7.69f, 0.0f, 76.2f, 0.0f, 0.777f, 4.15f, 1.17f}},
-    {2, 1, 1, 0, 256, {6.79f, 0.0f, 17.0f, 1.88f, 0.676f, 2.97f, 2.47f}},
-    {2, 1, 1, 1, 256, {8.5f, 0.0f, 57.7f, 8.49f, 0.138f, 4.35f, 2.22f}},
+    {2, 1, 0, 0, 1536, {2.33f, 3.37f, 29.8f, 48.8f, 0.708f, 3.16f, 2.76f}},
+    {2, 1, 0, 1, 512, {8.58f, 0.0f, 62.7f, 29.3f, 0.431f, 3.62f, 1.74f}},
+    {2, 1, 1, 0, 512, {5.97f, 0.944f, 15.9f, 14.0f, 1.11f, 2.95f, 3.18f}},
+    {2, 1, 1, 1, 256, {8.81f, 2.47f, 33.5f, 10.3f, 0.632f, 3.7f, 2.26f}},
+    {2, 1, 1, 2, 256, {11.4f, 0.964f, 59.2f, 18.6f, 0.3f, 4.44f, 1.87f}},
     {3, 0, 0, 0, 1536, {6.62f, 0.0f, 9.87f, 18.1f, 0.397f, 2.33f, 2.54f}},
     {3, 0, 0, 1, 768, {9.12f, 0.0f, 16.4f, 19.7f, 0.362f, 3.69f, 1.4f}},
     {3, 0, 1, 0, 512, {5.56f, 1.34f, 3.94f, 5.76f, 0.476f, 2.8f, 2.89f}},
     {3, 0, 1, 1, 256, {5.9f, 2.99f, 7.42f, 3.96f, 0.336f, 4.43f, 1.74f}},
     {3, 0, 1, 2, 256, {7.05f, 1.96f, 10.5f, 7.67f, 0.35f, 5.19f, 1.39f}},
     {3, 0, 1, 3, 256, {8.06f, 3.53f, 17.1f, 13.5f, 0.227f, 6.23f, 1.06f}},
-    {3, 1, 0, 0, 1536, {5.45f, 0.0f, 26.5f, 99.4f, 0.553f, 2.66f, 2.28f}},
-    {3, 1, 0, 1, 256, {8.31f, 0.0f, 75.8f, 1.78f, 0.473f, 4.59f, 1.09f}},
-    {3, 1, 1, 0, 256, {5.74f, 0.608f, 17.4f, 3.12f, 0.575f, 2.99f, 2.14f}},
-    {3, 1, 1, 1, 256, {6.12f, 1.75f, 58.2f, 13.0f, 0.623f, 5.07f, 1.69f}},
+    {3, 1, 0, 0, 1536, {6.03f, 0.0f, 30.0f, 69.5f, 0.569f, 2.96f, 2.23f}},
+    {3, 1, 0, 1, 512, {9.02f, 0.0f, 60.8f, 41.9f, 0.6f, 4.1f, 1.36f}},
+    {3, 1, 1, 0, 512, {5.38f, 1.29f, 16.9f, 16.1f, 0.946f, 3.34f, 2.54f}},
+    {3, 1, 1, 1, 256, {6.55f, 4.24f, 36.2f, 12.9f, 0.626f, 4.94f, 1.45f}},
+    {3, 1, 1, 2, 256, {8.34f, 3.51f, 63.1f, 21.4f, 0.593f, 6.24f, 1.18f}},
 };
+
+// one product of a model's kind
+struct DenseShape {
+    const DenseModel& m;
+    double k, sums;
+    long long tiles, padded;
+    int stages;
+    DenseShape(const DenseModel& model, int M, int N, int stages_) : m(model), stages(stages_) {
+        static const int kRows[] = {64, 128, 256, 256}, kCols[] = {64, 128, 128, 256}, kPairCols[] = {64, 64, 64, 128};
+        const bool pair = m.kind == kDensePair;
+        const long long bm = kRows[m.tile], bn = (pair ? kPairCols : kCols)[m.tile];
+        tiles = ((M + bm - 1) / bm) * ((N + bn - 1) / bn), padded = (tiles + kXcds - 1) / kXcds * kXcds;
+        k = 1e-3 * stages * (m.f32 ? 32 : 64), sums = 1e-6 * M * N * (pair ? 2 : 1);
+    }
+    // two stages to a part, parts side by side
+    bool allowed(int parts) const { return parts == 1 || (parts * 2 <= stages && tiles * parts <= (m.direct ? 560 : 1200)); }
+    double groups(int parts) const { return (double)(parts > 1 ? padded * parts : tiles); }
+    double us(int parts) const {
+        const double g = groups(parts);
+        return m.us[0] + std::ceil(g / m.slots) * (m.us[1] + m.us[2] * k / parts) + g / m.slots * m.us[3] * k / parts + m.us[4] * sums + (parts > 1 ? m.us[5] + m.us[6] * parts * sums : 0.0);
+    }
+};
+
+static DensePlan fastest(DenseKind kind, int M, int N, int stages, bool f32, bool direct, int tile, double* best_us) {
+    DensePlan best{kTileS, 1};
+    *best_us = 0.0;
+    for (const DenseModel& m : kDenseModels) {
+        if (m.kind != (int)kind || m.f32 != f32 || m.direct != direct || (tile >= 0 && m.tile != tile)) continue;
+        const DenseShape shape(m, M, N, stages);
+        for (int parts = 1; parts <= 16 && shape.allowed(parts); ++parts) {
+            const double us = shape.us(parts);
+            if (*best_us == 0.0 || us < *best_us) best = {m.tile, parts}, *best_us = us;
+        }
+    }
+    return best;
+}
 
 DensePlan plan_dense(DenseKind kind, int M, int N, int stages, bool f32, bool direct) {
     if (M <= 0 || N <= 0) return {kTileS, 1};
     struct Key { int32_t M, N, stages, form; };
     static thread_local DecisionCache<Key, DensePlan, 64> cache;
     return cache.get(Key{M, N, stages, f32 + 2 * direct + 4 * (int)kind}, [&] {
-        DensePlan best{kTileS, 1};
-        double best_us = 0.0;
-        const bool pair = kind == kDensePair;
-        const double k = 1e-3 * stages * (f32 ? 32 : 64), sums = 1e-6 * M * N * (pair ? 2 : 1);
-        for (const DenseModel& m : kDenseModels) {
-            if (m.kind != (int)kind || m.f32 != f32 || m.direct != direct) continue;
-            static const int kRows[] = {64, 128, 256, 256}, kCols[] = {64, 128, 128, 256}, kPairCols[] = {64, 64, 64, 128};
-            const long long bm = kRows[m.tile], bn = (pair ? kPairCols : kCols)[m.tile];
-            const long long tiles = ((M + bm - 1) / bm) * ((N + bn - 1) / bn), padded = (tiles + kXcds - 1) / kXcds * kXcds;
-            for (int parts = 1; parts <= 16; ++parts) {
-                if (parts > 1 && (parts * 2 > stages || tiles * parts > (direct ? 560 : 1200))) break;   // two stages to a part, parts side by side
-                const double groups = (double)(parts > 1 ? padded * parts : tiles), rounds = std::ceil(groups / m.slots);
-                const double us = m.us[0] + rounds * (m.us[1] + m.us[2] * k / parts) + groups / m.slots * m.us[3] * k / parts + m.us[4] * sums +
-                                  (parts > 1 ? m.us[5] + m.us[6] * parts * sums : 0.0);
-                if (best_us == 0.0 || us < best_us) best = {m.tile, parts}, best_us = us;
-            }
+        double us;
+        return fastest(kind, M, N, stages, f32, direct, -1, &us);
+    });
+}
+
+// Two products in one launch, fitted likewise to 69000 timings of 5500 pairs: fixed, a round; by 1000 elements of K a round of the mean workgroup, the work of all of them and the longest one; results; second, part.
+struct DenseTwoModel {
+    int f32, direct, tile, slots;
+    float us[8];
+};
+static const DenseTwoModel kDenseTwoModels[] = {
+    {0, 0, 0, 512, {5.3f, 0.413f, 0.528f, 4.79f, 10.6f, 0.0f, 3.59f, 2.04f}},
+    {0, 0, 1, 1024, {7.29f, 1.09f, 1.8f, 22.2f, 15.5f, 0.0f, 4.11f, 1.47f}},
+    {0, 1, 0, 512, {6.35f, 1.39f, 0.0f, 7.46f, 2.65f, 0.0f, 2.67f, 2.57f}},
+    {0, 1, 1, 256, {7.64f, 2.42f, 1.33f, 6.54f, 4.41f, 0.0f, 3.31f, 1.83f}},
+    {0, 1, 2, 256, {7.99f, 1.77f, 2.51f, 8.62f, 7.4f, 0.0f, 3.85f, 1.49f}},
+    {0, 1, 3, 256, {8.68f, 3.1f, 2.18f, 13.2f, 14.5f, 0.0f, 4.75f, 1.24f}},
+    {1, 0, 0, 1536, {4.65f, 0.996f, 0.809f, 57.2f, 29.0f, 0.0f, 3.24f, 2.52f}},
+    {1, 0, 1, 512, {5.78f, 2.25f, 6.13f, 41.6f, 59.0f, 0.0f, 3.81f, 1.62f}},
+    {1, 1, 0, 512, {6.26f, 1.5f, 0.728f, 20.5f, 14.0f, 0.0f, 2.69f, 2.66f}},
+    {1, 1, 1, 256, {8.47f, 3.63f, 5.47f, 20.0f, 28.7f, 0.0f, 3.18f, 1.76f}},
+    {1, 1, 2, 256, {7.66f, 4.93f, 8.66f, 28.0f, 53.5f, 0.0f, 4.34f, 1.34f}},
+};
+
+// One launch where it is expected to be ahead of two: on 9 of 10 of those pairs, by 20 % of both products on average (2 to 6 % behind the best tile and parts).
+DensePlans plan_gradients(int B, int d_in, int K_stages, int rows, int B_stages, bool f32, bool direct) {
+    struct Key { int32_t B, d_in, K_stages, rows, B_stages, form; };
+    static thread_local DecisionCache<Key, DensePlans, 64> cache;
+    if (B <= 0 || d_in <= 0 || rows <= 0) return {{kTileS, 1}, {kTileS, 1}, false};
+    return cache.get(Key{B, d_in, K_stages, rows, B_stages, f32 + 2 * direct}, [&] {
+        DensePlans best{};
+        double us_x, us_W;
+        best.dx = fastest(kDenseGradX, B, d_in, K_stages, f32, direct, -1, &us_x);
+        best.dW = fastest(kDenseGradW, rows, d_in, B_stages, f32, direct, -1, &us_W);
+        double best_us = us_x + us_W;
+        for (const DenseTwoModel& m : kDenseTwoModels) {
+            if (m.f32 != f32 || m.direct != direct) continue;
+            const DenseModel shape_of{kDenseGradX, f32, direct, m.tile, m.slots, {}};
+            const DenseShape x(shape_of, B, d_in, K_stages), W(shape_of, rows, d_in, B_stages);
+            for (int a = 1; a <= 16 && x.allowed(a); ++a)
+                for (int b = 1; b <= 16 && W.allowed(b); ++b) {
+                    const double gx = (double)x.padded * a, gW = (double)W.padded * b, work = gx * x.k / a + gW * W.k / b;
+                    const double us = m.us[0] + std::ceil((gx + gW) / m.slots) * (m.us[1] + m.us[2] * work / (gx + gW)) + m.us[3] * work / m.slots + m.us[4] * std::max(x.k / a, W.k / b) +
+                                      m.us[5] * (x.sums + W.sums) + (a > 1 || b > 1 ? m.us[6] : 0.0) + m.us[7] * ((a > 1 ? a * x.sums : 0.0) + (b > 1 ? b * W.sums : 0.0));
+                    if (us < best_us) best = {{m.tile, a}, {m.tile, b}, true}, best_us = us;
+                }
         }
         return best;
     });
@@ -233,7 +303,7 @@ static srigl_status linear_act(const void* x, int B, int d_in, const void* Wd, c
     const RowsOf<T> a{(const T*)x, d_in, B - 1, d_in}, w{(const T*)Wd, d_in, n - 1, d_in};
     const LinearOut<T, TY> out{n == d_out ? nullptr : active, n, bias, (const TY*)residual, d_out, (TY*)y, (T*)z, act, {}};
     if (few) return launch_few<T, false>((const T*)x, B, d_in, (const T*)Wd, 0, n, out, st);
-    return launch_dense<T, false>(a, w, B, n, stages_of<T>(d_in), plan, out, (float*)ws, st);
+    return launch_dense<T, false>(DenseProduct<RowsOf<T>, RowsOf<T>, LinearOut<T, TY>>{a, w, out, B, n, stages_of<T>(d_in), plan.parts, (float*)ws}, plan.tile, st);
 }
 
 template <typename T>
@@ -246,7 +316,7 @@ static srigl_status gated(const void* x, int B, int d_in, const void* Wg, const 
     const PairedRows<T, 32> w{(const T*)Wg, bytes_between(Wg, Wu), d_in, n - 1, d_in};
     const GatedOut<T> out{bias_g, bias_u, n, (T*)h, (T*)g, (T*)u, act, {}, {}};
     if (few) return launch_few<T, true>((const T*)x, B, d_in, (const T*)Wg, bytes_between(Wg, Wu), n, out, st);
-    return launch_dense<T, true>(a, w, B, n, stages_of<T>(d_in), plan, out, (float*)ws, st);
+    return launch_dense<T, true>(DenseProduct<RowsOf<T>, PairedRows<T, 32>, GatedOut<T>>{a, w, out, B, n, stages_of<T>(d_in), plan.parts, (float*)ws}, plan.tile, st);
 }
 
 }  // namespace srigl

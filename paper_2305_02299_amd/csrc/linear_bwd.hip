@@ -186,8 +186,8 @@ struct TwoOut {
 // What a backward pass takes of the workspace
 struct BwdPlan {
     int chunk_rows, chunks;
-    DensePlan dx, dW;
-    size_t dz_bytes, sum_bytes, bytes;   // the products' parts lie behind both
+    DensePlans products;
+    size_t dz_bytes, sum_bytes, dx_part_bytes, bytes;   // in this order, the parts of dW's product last
 };
 static size_t whole(size_t bytes) { return (bytes + 255) / 256 * 256; }
 // cols: columns of dz in a row, padding included; K: what dx's product sums over; dW_rows: rows of the weight gradients' product; sum_cols: columns of the sums
@@ -204,10 +204,17 @@ static BwdPlan plan_bwd(int B, int d_in, long long cols, long long K, long long 
     p.dz_bytes = whole((size_t)B * cols * elem);
     p.sum_bytes = whole((size_t)p.chunks * sum_cols * sizeof(float));
     const auto stages = [&](long long K) { return f32 ? stages_of<float>(K) : stages_of<uint16_t>(K); };
-    p.dx = plan_dense(kDenseGradX, B, d_in, stages(K), f32, direct);
-    p.dW = plan_dense(kDenseGradW, (int)dW_rows, d_in, stages(B), f32, direct);
-    p.bytes = p.dz_bytes + p.sum_bytes + whole(std::max(part_bytes(p.dx, B, d_in, false), part_bytes(p.dW, (int)dW_rows, d_in, false)));
+    p.products = plan_gradients(B, d_in, stages(K), (int)dW_rows, stages(B), f32, direct);
+    p.dx_part_bytes = whole(part_bytes(p.products.dx, B, d_in, false));
+    p.bytes = p.dz_bytes + p.sum_bytes + p.dx_part_bytes + whole(part_bytes(p.products.dW, (int)dW_rows, d_in, false));
     return p;
+}
+
+template <typename T, class P, class Q>
+static srigl_status launch_gradients(const DensePlans& plans, const P& of_x, bool want_x, const Q& of_W, bool want_W, hipStream_t st) {
+    if (want_x && want_W && plans.together && of_x.M > 0 && of_W.M > 0) return launch_dense_two<T>(of_x, of_W, plans.dx.tile, st);
+    const srigl_status rc = want_x ? launch_dense<T, false>(of_x, plans.dx.tile, st) : SRIGL_OK;
+    return rc == SRIGL_OK && want_W ? launch_dense<T, false>(of_W, plans.dW.tile, st) : rc;
 }
 
 template <typename T, typename TY>
@@ -216,7 +223,7 @@ static srigl_status linear_bwd(const BwdPlan& p, const void* dy, const void* x, 
     const int pitch = (int)padded(n);
     const int32_t* const list = n == d_out ? nullptr : active;
     T* const dz = reinterpret_cast<T*>(ws);
-    float *const sums = reinterpret_cast<float*>(ws + p.dz_bytes), *const part = reinterpret_cast<float*>(ws + p.dz_bytes + p.sum_bytes);
+    float *const sums = reinterpret_cast<float*>(ws + p.dz_bytes), *const dx_part = reinterpret_cast<float*>(ws + p.dz_bytes + p.sum_bytes), *const dW_part = reinterpret_cast<float*>(ws + p.dz_bytes + p.sum_bytes + p.dx_part_bytes);
     // without an activation or ablated neurons dz is dy: only its column sums are left to do
     const bool as_it_is = std::is_same<T, TY>::value && act == SRIGL_ACT_NONE && !list && n % kPiece<T> == 0 && !astray(16, {dy});
     if (p.chunks > 0 && n > 0 && (!as_it_is || dbias)) {
@@ -232,17 +239,10 @@ static srigl_status linear_bwd(const BwdPlan& p, const void* dy, const void* x, 
     }
     const T* const d = as_it_is ? (const T*)dy : dz;
     const int d_pitch = as_it_is ? n : pitch;
-    srigl_status rc = hip_ok(hipGetLastError());
-    if (rc == SRIGL_OK && dx) {
-        const RowsOf<T> a{d, d_pitch, B - 1, d_pitch};
-        const ColsOf<T> w{(const T*)Wd, d_in, d_in, n};
-        rc = launch_dense<T, false>(a, w, B, d_in, stages_of<T>(n), p.dx, PlainOut<T>{(T*)dx, d_in}, part, st);
-    }
-    if (rc == SRIGL_OK && dWd) {
-        const ColsOf<T> a{d, d_pitch, d_pitch, B}, b{(const T*)x, d_in, d_in, B};
-        rc = launch_dense<T, false>(a, b, n, d_in, stages_of<T>(B), p.dW, PlainOut<T>{(T*)dWd, d_in}, part, st);
-    }
-    return rc;
+    if (hip_ok(hipGetLastError()) != SRIGL_OK) return SRIGL_ERR_HIP;
+    const DenseProduct<RowsOf<T>, ColsOf<T>, PlainOut<T>> of_x{{d, d_pitch, B - 1, d_pitch}, {(const T*)Wd, d_in, d_in, n}, {(T*)dx, d_in}, B, d_in, stages_of<T>(n), p.products.dx.parts, dx_part};
+    const DenseProduct<ColsOf<T>, ColsOf<T>, PlainOut<T>> of_W{{d, d_pitch, d_pitch, B}, {(const T*)x, d_in, d_in, B}, {(T*)dWd, d_in}, n, d_in, stages_of<T>(B), p.products.dW.parts, dW_part};
+    return launch_gradients<T>(p.products, of_x, dx != nullptr, of_W, dWd != nullptr, st);
 }
 
 template <typename T>
@@ -250,24 +250,19 @@ static srigl_status gated_bwd(const BwdPlan& p, const void* dh, const void* x, i
                               int act, void* dx, void* dWg, void* dWu, float* dbias_g, float* dbias_u, unsigned char* ws, hipStream_t st) {
     const int pitch = (int)padded(n);
     T* const dz = reinterpret_cast<T*>(ws);
-    float *const sums = reinterpret_cast<float*>(ws + p.dz_bytes), *const part = reinterpret_cast<float*>(ws + p.dz_bytes + p.sum_bytes);
+    float *const sums = reinterpret_cast<float*>(ws + p.dz_bytes), *const dx_part = reinterpret_cast<float*>(ws + p.dz_bytes + p.sum_bytes), *const dW_part = reinterpret_cast<float*>(ws + p.dz_bytes + p.sum_bytes + p.dx_part_bytes);
     const bool want_sums = dbias_g || dbias_u;
     if (p.chunks > 0 && n > 0)
         hipLaunchKernelGGL(k_dz_gated<T>, dim3((unsigned)((pitch + kDzCols * kPiece<T> - 1) / (kDzCols * kPiece<T>)), (unsigned)p.chunks), dim3(256), 0, st, (const T*)dh, (const T*)g, (const T*)u, n, B, act, dz,
                            pitch, want_sums ? sums : nullptr, p.chunk_rows);
     if (want_sums && n > 0)
         hipLaunchKernelGGL(k_sum_chunks, dim3((unsigned)((2ll * n + 63) / 64)), dim3(256), 0, st, sums, p.chunks, 2 * n, n, nullptr, n, nullptr, act, dbias_g, dbias_u);
-    srigl_status rc = hip_ok(hipGetLastError());
-    if (rc == SRIGL_OK && dx) {
-        const RowsOf<T> a{dz, 2ll * pitch, B - 1, 2 * pitch};
-        const PairedCols<T> w{(const T*)Wg, bytes_between(Wg, Wu), d_in, d_in, n, pitch};
-        rc = launch_dense<T, false>(a, w, B, d_in, stages_of<T>(2ll * pitch), p.dx, PlainOut<T>{(T*)dx, d_in}, part, st);
-    }
-    if (rc == SRIGL_OK && (dWg || dWu) && n > 0) {
-        const ColsOf<T> a{dz, 2ll * pitch, 2 * pitch, B}, b{(const T*)x, d_in, d_in, B};
-        rc = launch_dense<T, false>(a, b, 2 * pitch, d_in, stages_of<T>(B), p.dW, TwoOut<T>{(T*)dWg, (T*)dWu, d_in, n, pitch}, part, st);
-    }
-    return rc;
+    if (hip_ok(hipGetLastError()) != SRIGL_OK) return SRIGL_ERR_HIP;
+    const DenseProduct<RowsOf<T>, PairedCols<T>, PlainOut<T>> of_x{{dz, 2ll * pitch, B - 1, 2 * pitch}, {(const T*)Wg, bytes_between(Wg, Wu), d_in, d_in, n, pitch}, {(T*)dx, d_in}, B, d_in,
+                                                                  stages_of<T>(2ll * pitch), p.products.dx.parts, dx_part};
+    const DenseProduct<ColsOf<T>, ColsOf<T>, TwoOut<T>> of_W{{dz, 2ll * pitch, 2 * pitch, B}, {(const T*)x, d_in, d_in, B}, {(T*)dWg, (T*)dWu, d_in, n, pitch}, 2 * pitch, d_in, stages_of<T>(B),
+                                                            p.products.dW.parts, dW_part};
+    return launch_gradients<T>(p.products, of_x, dx != nullptr, of_W, dWg || dWu, st);
 }
 
 static bool bwd_sizes_fit(int B, int d_in, int d_out) { return B <= kMaxSide && d_in <= kMaxSide && d_out <= kMaxSide / 2; }
