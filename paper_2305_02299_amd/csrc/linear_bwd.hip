@@ -43,29 +43,19 @@ __device__ __forceinline__ void sum_row_lanes(float (*held)[kDzCols * V], float 
             for (int r = 1; r < kDzRows; ++r) v[q] += held[r][q * kDzCols + cg];
 }
 
-// dz[B][pitch] (pitch: n_active padded with zeros) and, per chunk of rows, the sums of its columns in sums[chunk][d_out] at the neurons' columns.  dz or sums: nullptr where not wanted.
-template <typename T, typename TY, bool LISTED>
-__global__ __launch_bounds__(256) void k_dz_linear(const TY* __restrict__ dy, const T* __restrict__ z, const int32_t* __restrict__ active, int n, int B, int d_out, int act,
-                                                  T* __restrict__ dz, int pitch, float* __restrict__ sums, int rows) {
+// dz[B][pitch] (pitch: n padded with zeros) and, per chunk of rows, its column sums in sums[chunk][n].  dz or sums: nullptr where not wanted.
+template <typename T, typename TY>
+__global__ __launch_bounds__(256) void k_dz_linear(const TY* __restrict__ dy, const T* __restrict__ z, int n, int B, int act, T* __restrict__ dz, int pitch,
+                                                  float* __restrict__ sums, int rows) {
     constexpr int V = kPiece<T>;
     __shared__ float held[kDzRows][kDzCols * V];
     const int s = (int)((blockIdx.x * (unsigned)kDzCols + threadIdx.x % kDzCols) * V), m0 = blockIdx.y * rows, m1 = min(m0 + rows, B), valid = n - s;
-    int col[V];
-    if constexpr (LISTED)
-#pragma unroll
-        for (int q = 0; q < V; ++q) {
-            col[q] = q < valid ? active[s + q] : -1;
-            if ((unsigned)col[q] >= (unsigned)d_out) col[q] = -1;
-        }
     float sum[V] = {};
     if (s < pitch)
         for (int m = m0 + threadIdx.x / kDzCols; m < m1; m += kDzRows) {
             float v[V] = {}, zv[V] = {};
             if (valid > 0) {
-                if constexpr (LISTED)
-#pragma unroll
-                    for (int q = 0; q < V; ++q) v[q] = col[q] >= 0 ? to_float(dy[(size_t)m * d_out + col[q]]) : 0.0f;
-                else load_values<TY, V>(dy + (size_t)m * d_out + s, v, valid);
+                load_values<TY, V>(dy + (size_t)m * n + s, v, valid);
                 if (act != SRIGL_ACT_NONE) {
                     load_values<T, V>(z + (size_t)m * n + s, zv, valid);
 #pragma unroll
@@ -78,25 +68,66 @@ __global__ __launch_bounds__(256) void k_dz_linear(const TY* __restrict__ dy, co
         }
     if (!sums) return;
     sum_row_lanes<V>(held, sum);
-    if (threadIdx.x / kDzCols == 0)
-#pragma unroll
-        for (int q = 0; q < V; ++q) {
-            const int c = LISTED ? (q < valid ? col[q] : -1) : (q < valid ? s + q : -1);
-            if (c >= 0) sums[(size_t)blockIdx.y * d_out + c] = sum[q];
-        }
+    if (threadIdx.x / kDzCols == 0 && valid > 0) store_values<float, V>(sums + (size_t)blockIdx.y * n + s, sum, valid);
 }
 
-// The same chunks' sums of dy in the ablated columns
-template <typename TY>
-__global__ __launch_bounds__(256) void k_ablated_sums(const TY* __restrict__ dy, const int32_t* __restrict__ active, int n, int B, int d_out, float* __restrict__ sums, int rows) {
-    const int c = blockIdx.x * 256 + threadIdx.x, m0 = blockIdx.y * rows, m1 = min(m0 + rows, B);
-    if (c >= d_out) return;
-    const int s = n ? place_of(active, n, c) : 0;
-    if (s < n && active[s] == c) return;
-    float v = 0.0f;
-#pragma unroll 8
-    for (int m = m0; m < m1; ++m) v += to_float(dy[(size_t)m * d_out + c]);
-    sums[(size_t)blockIdx.y * d_out + c] = v;
+// The same for a layer with ablated neurons: a workgroup takes 32 V columns of dy, whose stored neurons are consecutive ones.  A row of dy passes through the LDS, out of which a thread picks its V
+// neurons' values; ablated columns go into the sums as they are (sums[chunk][d_out]).  (Values picked out of memory one by one, and the ablated columns read again by a launch of their own: 99 us on 13108 of
+// 16384 neurons and 2048 rows in bf16.)
+template <typename T, typename TY>
+__global__ __launch_bounds__(256) void k_dz_listed(const TY* __restrict__ dy, const T* __restrict__ z, const int32_t* __restrict__ active, int n, int B, int d_out, int act,
+                                                  T* __restrict__ dz, int pitch, float* __restrict__ sums, int rows) {
+    constexpr int V = kPiece<T>, COLS = kDzCols * V;
+    __shared__ float row[2][kDzRows][COLS], held[kDzRows][COLS];
+    __shared__ int stored[COLS];
+    const int cg = threadIdx.x % kDzCols, rl = threadIdx.x / kDzCols, c0 = blockIdx.x * COLS, c = c0 + cg * V, m0 = blockIdx.y * rows, m1 = min(m0 + rows, B);
+    const int s0 = place_of(active, n, c0), s1 = min(place_of(active, n, min(c0 + COLS, d_out)), s0 + COLS), s = s0 + cg * V, count = s1 - s, there = d_out - c;
+    int pick[V];   // where in the row the thread's neurons stand
+    for (int k = threadIdx.x; k < COLS; k += 256) stored[k] = 0;
+    __syncthreads();
+#pragma unroll
+    for (int q = 0; q < V; ++q) {
+        pick[q] = q < count ? active[s + q] - c0 : -1;
+        if ((unsigned)pick[q] >= (unsigned)COLS) pick[q] = -1;
+        if (pick[q] >= 0) stored[pick[q]] = 1;
+    }
+    float sum[V] = {}, passed[V] = {};
+    int buffer = 0;
+    for (int base = m0; base < m1; base += kDzRows, buffer ^= 1) {
+        const int m = base + rl;
+        float v[V] = {}, zv[V] = {};
+        if (m < m1 && there > 0) load_values<TY, V>(dy + (size_t)m * d_out + c, v, there);
+        if (m < m1 && count > 0 && act != SRIGL_ACT_NONE) load_values<T, V>(z + (size_t)m * n + s, zv, count);
+#pragma unroll
+        for (int q = 0; q < V; ++q) {
+            passed[q] += v[q];
+            row[buffer][rl][cg * V + q] = v[q];
+        }
+        __syncthreads();   // (the other buffer is written next: one barrier a row)
+        if (m < m1 && count > 0) {
+#pragma unroll
+            for (int q = 0; q < V; ++q) {
+                v[q] = pick[q] >= 0 ? row[buffer][rl][pick[q]] : 0.0f;
+                if (act != SRIGL_ACT_NONE && pick[q] >= 0) v[q] *= act_slope(zv[q], act);
+                sum[q] += v[q];
+            }
+            if (dz) store_values<T, V>(dz + (size_t)m * pitch + s, v, count);
+        }
+    }
+    if (dz && s1 == n && c0 + COLS >= d_out)   // the last workgroup: the padding
+        for (int m = m0 + rl; m < m1; m += kDzRows)
+            for (int k = n + cg; k < pitch; k += kDzCols) dz[(size_t)m * pitch + k] = 0;
+    if (!sums) return;
+    sum_row_lanes<V>(held, sum);
+    sum_row_lanes<V>(held, passed);
+    if (rl == 0) {
+        float* const to = sums + (size_t)blockIdx.y * d_out + c0;
+#pragma unroll
+        for (int q = 0; q < V; ++q) {
+            if (pick[q] >= 0) to[pick[q]] = sum[q];
+            if (c + q < d_out && !stored[cg * V + q]) to[cg * V + q] = passed[q];
+        }
+    }
 }
 
 // (dg | du)[B][2 pitch] and the column sums of both in sums[chunk][2 n]
@@ -166,7 +197,7 @@ struct PlainOut {
     T* y;
     int N;
     template <int V> __device__ void start(int, int) {}
-    template <int V> __device__ void row(int m, int c, int valid, float (&v)[V]) { store_values<T, V>(y + (size_t)m * N + c, v, valid); }
+    template <int V> __device__ void row(int m, int c, int valid, float (&v)[V]) { store_values<T, V, true>(y + (size_t)m * N + c, v, valid); }
 };
 // Rows [0, n) to one matrix, [padded, padded + n) to a second; nullptr: not wanted
 template <typename T>
@@ -179,7 +210,7 @@ struct TwoOut {
         const bool behind = m >= padded;
         const int r = behind ? m - padded : m;
         T* const to = behind ? second : first;
-        if (r < n && to) store_values<T, V>(to + (size_t)r * N + c, v, valid);
+        if (r < n && to) store_values<T, V, true>(to + (size_t)r * N + c, v, valid);
     }
 };
 
@@ -221,22 +252,23 @@ template <typename T, typename TY>
 static srigl_status linear_bwd(const BwdPlan& p, const void* dy, const void* x, int B, int d_in, const void* Wd, const int32_t* active, int n, const float* bias,
                                const void* z, int d_out, int act, void* dx, void* dWd, float* dbias, unsigned char* ws, hipStream_t st) {
     const int pitch = (int)padded(n);
-    const int32_t* const list = n == d_out ? nullptr : active;
     T* const dz = reinterpret_cast<T*>(ws);
     float *const sums = reinterpret_cast<float*>(ws + p.dz_bytes), *const dx_part = reinterpret_cast<float*>(ws + p.dz_bytes + p.sum_bytes), *const dW_part = reinterpret_cast<float*>(ws + p.dz_bytes + p.sum_bytes + p.dx_part_bytes);
     // without an activation or ablated neurons dz is dy: only its column sums are left to do
-    const bool as_it_is = std::is_same<T, TY>::value && act == SRIGL_ACT_NONE && !list && n % kPiece<T> == 0 && !astray(16, {dy});
-    if (p.chunks > 0 && n > 0 && (!as_it_is || dbias)) {
-        const dim3 grid((unsigned)((pitch + kDzCols * kPiece<T> - 1) / (kDzCols * kPiece<T>)), (unsigned)p.chunks);
-        T* const to = as_it_is ? nullptr : dz;
-        if (list) hipLaunchKernelGGL((k_dz_linear<T, TY, true>), grid, dim3(256), 0, st, (const TY*)dy, (const T*)z, list, n, B, d_out, act, to, pitch, dbias ? sums : nullptr, p.chunk_rows);
-        else hipLaunchKernelGGL((k_dz_linear<T, TY, false>), grid, dim3(256), 0, st, (const TY*)dy, (const T*)z, list, n, B, d_out, act, to, pitch, dbias ? sums : nullptr, p.chunk_rows);
+    const bool as_it_is = std::is_same<T, TY>::value && act == SRIGL_ACT_NONE && n == d_out && n % kPiece<T> == 0 && !astray(16, {dy});
+    const bool listed = n < d_out;
+    if (p.chunks > 0 && (n > 0 || dbias) && (!as_it_is || dbias)) {
+        constexpr int COLS = kDzCols * kPiece<T>;
+        T* const to = as_it_is || n == 0 ? nullptr : dz;
+        float* const sum_to = dbias ? sums : nullptr;
+        if (listed)
+            hipLaunchKernelGGL((k_dz_listed<T, TY>), dim3((unsigned)((d_out + COLS - 1) / COLS), (unsigned)p.chunks), dim3(256), 0, st, (const TY*)dy, (const T*)z, active, n, B, d_out, act, to, pitch,
+                               sum_to, p.chunk_rows);
+        else
+            hipLaunchKernelGGL((k_dz_linear<T, TY>), dim3((unsigned)((pitch + COLS - 1) / COLS), (unsigned)p.chunks), dim3(256), 0, st, (const TY*)dy, (const T*)z, n, B, act, to, pitch, sum_to,
+                               p.chunk_rows);
     }
-    if (dbias) {
-        if (p.chunks > 0 && n < d_out)
-            hipLaunchKernelGGL(k_ablated_sums<TY>, dim3((unsigned)((d_out + 255ll) / 256), (unsigned)p.chunks), dim3(256), 0, st, (const TY*)dy, list, n, B, d_out, sums, p.chunk_rows);
-        hipLaunchKernelGGL(k_sum_chunks, dim3((unsigned)((d_out + 63ll) / 64)), dim3(256), 0, st, sums, p.chunks, d_out, d_out, list, n, bias, act, dbias, nullptr);
-    }
+    if (dbias) hipLaunchKernelGGL(k_sum_chunks, dim3((unsigned)((d_out + 63ll) / 64)), dim3(256), 0, st, sums, p.chunks, d_out, d_out, active, n, bias, act, dbias, nullptr);
     const T* const d = as_it_is ? (const T*)dy : dz;
     const int d_pitch = as_it_is ? n : pitch;
     if (hip_ok(hipGetLastError()) != SRIGL_OK) return SRIGL_ERR_HIP;
