@@ -771,6 +771,30 @@ __device__ __forceinline__ float act_slope(float v, int act) {
     return 1.0f;
 }
 
+// The same of V values, the choice made once for all: with a branch a value their chains of instructions followed each other (bf16 4096 -> 16384 at 2048 rows, in
+// the epilogue: gated with SiLU 505 us, now 460, a layer with GELU 298 and 278)
+template <int V>
+__device__ __forceinline__ void act_values(float (&v)[V], int act) {
+    const auto each = [&](int kind) {
+#pragma unroll
+        for (int q = 0; q < V; ++q) v[q] = act_value(v[q], kind);
+    };
+    if (act == SRIGL_ACT_GELU) each(SRIGL_ACT_GELU);
+    else if (act == SRIGL_ACT_SILU) each(SRIGL_ACT_SILU);
+    else if (act == SRIGL_ACT_RELU) each(SRIGL_ACT_RELU);
+}
+template <int V>
+__device__ __forceinline__ void act_slopes(const float (&v)[V], float (&slope)[V], int act) {
+    const auto each = [&](int kind) {
+#pragma unroll
+        for (int q = 0; q < V; ++q) slope[q] = act_slope(v[q], kind);
+    };
+    if (act == SRIGL_ACT_GELU) each(SRIGL_ACT_GELU);
+    else if (act == SRIGL_ACT_SILU) each(SRIGL_ACT_SILU);
+    else if (act == SRIGL_ACT_RELU) each(SRIGL_ACT_RELU);
+    else each(SRIGL_ACT_NONE);
+}
+
 // ---- kernel and launch ----
 // Sums of a part of K, [parts][M][N] (of a pair: [parts][M][2 N], the second's behind the first's)
 struct PartOut {

@@ -194,9 +194,10 @@ struct LinearOut {
         const size_t at = (size_t)m * d_out + c;
         float r[V] = {};
         if (residual) load_values<TY, V>(residual + at, r, valid, first);
+        act_values<V>(v, act);
 #pragma unroll
         for (int q = 0; q < V; ++q) {
-            v[q] = gaps >> q & 1 ? flat[q] : act_value(v[q], act);
+            v[q] = gaps >> q & 1 ? flat[q] : v[q];
             if (residual) v[q] += r[q];
         }
         store_values<TY, V>(y + at, v, valid, first);
@@ -213,8 +214,7 @@ struct LinearOut {
 #pragma unroll
         for (int q = 0; q < V; ++q) v[q] += b[q];
         if (z) store_values<T, V>(z + (size_t)m * n_active + s, v, valid);
-#pragma unroll
-        for (int q = 0; q < V; ++q) v[q] = act_value(v[q], act);
+        act_values<V>(v, act);
         if (!active) {
             const size_t at = (size_t)m * d_out + s;
             if (residual) {
@@ -268,8 +268,9 @@ struct GatedOut {
             store_values<T, V>(g + at, v, valid);
             store_values<T, V>(u + at, w, valid);
         }
+        act_values<V>(v, act);
 #pragma unroll
-        for (int q = 0; q < V; ++q) v[q] = act_value(v[q], act) * w[q];
+        for (int q = 0; q < V; ++q) v[q] *= w[q];
         store_values<T, V>(h + at, v, valid);
     }
 };

@@ -57,9 +57,11 @@ __global__ __launch_bounds__(256) void k_dz_linear(const TY* __restrict__ dy, co
             if (valid > 0) {
                 load_values<TY, V>(dy + (size_t)m * n + s, v, valid);
                 if (act != SRIGL_ACT_NONE) {
+                    float slope[V];
                     load_values<T, V>(z + (size_t)m * n + s, zv, valid);
+                    act_slopes<V>(zv, slope, act);
 #pragma unroll
-                    for (int q = 0; q < V; ++q) v[q] = q < valid ? v[q] * act_slope(zv[q], act) : 0.0f;
+                    for (int q = 0; q < V; ++q) v[q] = q < valid ? v[q] * slope[q] : 0.0f;
                 }
             }
 #pragma unroll
@@ -71,61 +73,92 @@ __global__ __launch_bounds__(256) void k_dz_linear(const TY* __restrict__ dy, co
     if (threadIdx.x / kDzCols == 0 && valid > 0) store_values<float, V>(sums + (size_t)blockIdx.y * n + s, sum, valid);
 }
 
-// The same for a layer with ablated neurons: a workgroup takes 32 V columns of dy, whose stored neurons are consecutive ones.  A row of dy passes through the LDS, out of which a thread picks its V
-// neurons' values; ablated columns go into the sums as they are (sums[chunk][d_out]).  (Values picked out of memory one by one, and the ablated columns read again by a launch of their own: 99 us on 13108 of
-// 16384 neurons and 2048 rows in bf16.)
+// The same for a layer with ablated neurons.  A workgroup's columns of dy are those from behind the neuron in front of its own to its last one (the last workgroup's: to the end).  Where they fit, a row of
+// them passes through the LDS, out of which a thread picks its V neurons' values, and all columns' sums are taken on the way; else the values are picked out of memory and the ablated columns' sums
+// taken by a pass of their own.  Ablated columns go into sums[chunk][d_out] as they are.  (13108 of 16384 neurons, 2048 rows, bf16: 76 us; all picked out of memory and the ablated columns read again by
+// a launch of their own 94; windows of columns, whose first and last neurons share a piece of dz with the windows beside, 107.)
 template <typename T, typename TY>
 __global__ __launch_bounds__(256) void k_dz_listed(const TY* __restrict__ dy, const T* __restrict__ z, const int32_t* __restrict__ active, int n, int B, int d_out, int act,
                                                   T* __restrict__ dz, int pitch, float* __restrict__ sums, int rows) {
-    constexpr int V = kPiece<T>, COLS = kDzCols * V;
-    __shared__ float row[2][kDzRows][COLS], held[kDzRows][COLS];
-    __shared__ int stored[COLS];
-    const int cg = threadIdx.x % kDzCols, rl = threadIdx.x / kDzCols, c0 = blockIdx.x * COLS, c = c0 + cg * V, m0 = blockIdx.y * rows, m1 = min(m0 + rows, B);
-    const int s0 = place_of(active, n, c0), s1 = min(place_of(active, n, min(c0 + COLS, d_out)), s0 + COLS), s = s0 + cg * V, count = s1 - s, there = d_out - c;
-    int pick[V];   // where in the row the thread's neurons stand
-    for (int k = threadIdx.x; k < COLS; k += 256) stored[k] = 0;
+    constexpr int V = kPiece<T>, OWN = kDzCols * V, PIECES = 2 * kDzCols, ROOM = PIECES * V;
+    __shared__ float row[2][kDzRows][ROOM + 32], held[kDzRows][OWN];   // (column k of a row at k % V * PIECES + k / V; rows by turns half of the banks apart)
+    __shared__ int stored[ROOM];
+    const int cg = threadIdx.x % kDzCols, rl = threadIdx.x / kDzCols, m0 = blockIdx.y * rows, m1 = min(m0 + rows, B);
+    const int s_first = blockIdx.x * OWN, s_behind = min(s_first + OWN, n), s = s_first + cg * V, valid = n - s;
+    const int lo = s_first > 0 && s_first <= n ? max(active[s_first - 1] + 1, 0) : 0, hi = s_behind == n ? d_out : min(active[s_behind - 1] + 1, d_out), c0 = lo / V * V;
+    const bool through = hi - c0 <= ROOM;
+    int col[V], place[V];   // which columns the thread's neurons are, and where in the LDS they stand
+    for (int k = threadIdx.x; k < ROOM; k += 256) stored[k] = 0;
     __syncthreads();
 #pragma unroll
     for (int q = 0; q < V; ++q) {
-        pick[q] = q < count ? active[s + q] - c0 : -1;
-        if ((unsigned)pick[q] >= (unsigned)COLS) pick[q] = -1;
-        if (pick[q] >= 0) stored[pick[q]] = 1;
+        col[q] = q < valid ? active[s + q] : -1;
+        if (col[q] < lo || col[q] >= hi) col[q] = -1;
+        const int k = col[q] - c0;
+        place[q] = through && col[q] >= 0 ? k % V * PIECES + k / V : 0;
+        if (through && col[q] >= 0) stored[k] = 1;
     }
-    float sum[V] = {}, passed[V] = {};
+    float sum[V] = {}, passed[2][V] = {};
     int buffer = 0;
     for (int base = m0; base < m1; base += kDzRows, buffer ^= 1) {
         const int m = base + rl;
-        float v[V] = {}, zv[V] = {};
-        if (m < m1 && there > 0) load_values<TY, V>(dy + (size_t)m * d_out + c, v, there);
-        if (m < m1 && count > 0 && act != SRIGL_ACT_NONE) load_values<T, V>(z + (size_t)m * n + s, zv, count);
+        const bool there = m < m1;
+        float v[V] = {}, zv[V] = {}, slope[V];
+        if (there && valid > 0 && act != SRIGL_ACT_NONE) load_values<T, V>(z + (size_t)m * n + s, zv, valid);
+        if (through) {
 #pragma unroll
-        for (int q = 0; q < V; ++q) {
-            passed[q] += v[q];
-            row[buffer][rl][cg * V + q] = v[q];
-        }
-        __syncthreads();   // (the other buffer is written next: one barrier a row)
-        if (m < m1 && count > 0) {
+            for (int j = 0; j < 2; ++j) {
+                const int c = c0 + (j * kDzCols + cg) * V;
+                float w[V] = {};
+                if (there && c < hi) load_values<TY, V>(dy + (size_t)m * d_out + c, w, d_out - c);
 #pragma unroll
-            for (int q = 0; q < V; ++q) {
-                v[q] = pick[q] >= 0 ? row[buffer][rl][pick[q]] : 0.0f;
-                if (act != SRIGL_ACT_NONE && pick[q] >= 0) v[q] *= act_slope(zv[q], act);
-                sum[q] += v[q];
+                for (int q = 0; q < V; ++q) {
+                    passed[j][q] += w[q];
+                    row[buffer][rl][q * PIECES + j * kDzCols + cg + (rl & 1) * 32] = w[q];
+                }
             }
-            if (dz) store_values<T, V>(dz + (size_t)m * pitch + s, v, count);
+            __syncthreads();   // (the other buffer is written next: one barrier a row)
+#pragma unroll
+            for (int q = 0; q < V; ++q) v[q] = row[buffer][rl][place[q] + (rl & 1) * 32];
+        } else if (there) {
+#pragma unroll
+            for (int q = 0; q < V; ++q) v[q] = to_float(dy[(size_t)m * d_out + max(col[q], 0)]);
         }
-    }
-    if (dz && s1 == n && c0 + COLS >= d_out)   // the last workgroup: the padding
-        for (int m = m0 + rl; m < m1; m += kDzRows)
-            for (int k = n + cg; k < pitch; k += kDzCols) dz[(size_t)m * pitch + k] = 0;
-    if (!sums) return;
-    sum_row_lanes<V>(held, sum);
-    sum_row_lanes<V>(held, passed);
-    if (rl == 0) {
-        float* const to = sums + (size_t)blockIdx.y * d_out + c0;
+        if (!there || s >= pitch) continue;
+        act_slopes<V>(zv, slope, act);
 #pragma unroll
         for (int q = 0; q < V; ++q) {
-            if (pick[q] >= 0) to[pick[q]] = sum[q];
-            if (c + q < d_out && !stored[cg * V + q]) to[cg * V + q] = passed[q];
+            v[q] = col[q] >= 0 ? v[q] * slope[q] : 0.0f;
+            sum[q] += v[q];
+        }
+        if (dz) store_values<T, V>(dz + (size_t)m * pitch + s, v, V);
+    }
+    if (!sums) return;
+    float* const to = sums + (size_t)blockIdx.y * d_out;
+    sum_row_lanes<V>(held, sum);
+    if (rl == 0)
+#pragma unroll
+        for (int q = 0; q < V; ++q)
+            if (col[q] >= 0) to[col[q]] = sum[q];
+    if (through) {
+#pragma unroll
+        for (int j = 0; j < 2; ++j) {
+            sum_row_lanes<V>(held, passed[j]);
+            if (rl == 0)
+#pragma unroll
+                for (int q = 0; q < V; ++q) {
+                    const int k = (j * kDzCols + cg) * V + q;
+                    if (c0 + k >= lo && c0 + k < hi && !stored[k]) to[c0 + k] = passed[j][q];
+                }
+        }
+    } else {
+        for (int c = lo + (int)threadIdx.x; c < hi; c += 256) {
+            const int at = n ? place_of(active, n, c) : 0;
+            if (at < n && active[at] == c) continue;
+            float v = 0.0f;
+#pragma unroll 8
+            for (int m = m0; m < m1; ++m) v += to_float(dy[(size_t)m * d_out + c]);
+            to[c] = v;
         }
     }
 }
@@ -146,9 +179,12 @@ __global__ __launch_bounds__(256) void k_dz_gated(const T* __restrict__ dh, cons
                 load_values<T, V>(dh + at, d, valid);
                 load_values<T, V>(g + at, gv, valid);
                 load_values<T, V>(u + at, uv, valid);
+                float slope[V];
+                act_slopes<V>(gv, slope, act);
+                act_values<V>(gv, act);
 #pragma unroll
                 for (int q = 0; q < V; ++q) {
-                    const float dg = d[q] * uv[q] * act_slope(gv[q], act), du = d[q] * act_value(gv[q], act);
+                    const float dg = d[q] * uv[q] * slope[q], du = d[q] * gv[q];
                     gv[q] = q < valid ? dg : 0.0f;
                     uv[q] = q < valid ? du : 0.0f;
                     sg[q] += gv[q];
@@ -262,7 +298,7 @@ static srigl_status linear_bwd(const BwdPlan& p, const void* dy, const void* x, 
         T* const to = as_it_is || n == 0 ? nullptr : dz;
         float* const sum_to = dbias ? sums : nullptr;
         if (listed)
-            hipLaunchKernelGGL((k_dz_listed<T, TY>), dim3((unsigned)((d_out + COLS - 1) / COLS), (unsigned)p.chunks), dim3(256), 0, st, (const TY*)dy, (const T*)z, active, n, B, d_out, act, to, pitch,
+            hipLaunchKernelGGL((k_dz_listed<T, TY>), dim3((unsigned)std::max(1, (pitch + COLS - 1) / COLS), (unsigned)p.chunks), dim3(256), 0, st, (const TY*)dy, (const T*)z, active, n, B, d_out, act, to, pitch,
                                sum_to, p.chunk_rows);
         else
             hipLaunchKernelGGL((k_dz_linear<T, TY>), dim3((unsigned)((pitch + COLS - 1) / COLS), (unsigned)p.chunks), dim3(256), 0, st, (const TY*)dy, (const T*)z, n, B, act, to, pitch, sum_to,
