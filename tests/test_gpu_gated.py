@@ -208,6 +208,51 @@ def test_a_block_on_a_side_stream_and_in_graphs():
             assert all(torch.equal(a, b) for a, b in zip(outs, eager)) and all(torch.equal(a, b) for a, b in zip(again, eager))
 
 
+def test_one_bias_alone_and_one_matrix_twice():
+    gen = torch.Generator().manual_seed(9)
+    W, x, bias, dh = whole(gen, (50, 24), 2), whole(gen, (20, 24), 2), whole(gen, (50,), 2), whole(gen, (20, 50), 2)
+    for first in (True, False):
+        block = GatedLinear(24, 50, W.cuda(), W.cuda(), bias.cuda() if first else None, None if first else bias.cuda(), B_.ACT_RELU)
+        h, g, u = block.forward(x.cuda(), save=True)
+        p = x.double() @ W.double().T
+        wg, wu = (p + bias, p) if first else (p, p + bias)
+        assert torch.equal(g.cpu().double(), wg) and torch.equal(u.cpu().double(), wu) and torch.equal(h.cpu().double(), wg.clamp(min=0) * wu)
+        out = block.backward(dh.cuda(), x.cuda(), g, u)
+        assert (out[3] is not None) == first and (out[4] is None) == first
+        dg, du = dh.double() * wu * (wg > 0), dh.double() * wg.clamp(min=0)
+        assert torch.equal((out[3] if first else out[4]).cpu().double(), (dg if first else du).sum(0))
+        assert torch.equal(out[0].cpu().double(), (dg + du) @ W.double())
+
+
+@pytest.mark.parametrize("B,d_in,n", [(70000, 8, 5), (3, 16, 70001), (100, 0, 70), (33, 1003, 4099)])
+def test_more_rows_or_neurons_than_a_grid_has_lines(B, d_in, n):
+    gen, t = torch.Generator().manual_seed(B), torch.bfloat16
+    block, Wg, Wu, bg, bu = _block(gen, d_in, n, t, lambda s, tt: whole(gen, s, 1, tt), True, "relu")
+    x, dh = whole(gen, (B, d_in), 1, t), whole(gen, (B, n), 1, t)
+    g, u = (linear(x, W, torch.arange(n), b, n, "none")[2] for W, b in ((Wg, bg), (Wu, bu)))
+    assert torch.equal(block.forward(x.cuda()).cpu(), (g.clamp(min=0) * u).to(t))
+    gs, us = whole(gen, (B, n), 2, t), whole(gen, (B, n), 2, t)
+    dg, du = dh.double() * us.double() * (gs > 0), dh.double() * gs.double().clamp(min=0)
+    dx, dWg, dWu, dbg, dbu = block.backward(dh.cuda(), x.cuda(), gs.cuda(), us.cuda())
+    assert torch.equal(dx.cpu(), (dg @ Wg.double() + du @ Wu.double()).to(t)) and torch.equal(dWg.cpu(), (dg.T @ x.double()).to(t))
+    assert torch.equal(dWu.cpu(), (du.T @ x.double()).to(t)) and torch.equal(dbg.cpu(), dg.sum(0).float()) and torch.equal(dbu.cpu(), du.sum(0).float())
+
+
+def test_results_beyond_32_bits():
+    """More than 2^32 bytes and 2^31 elements of results: the last rows are what the same rows give by themselves."""
+    B, d_in, n = 280000, 64, 8192
+    gen = torch.Generator().manual_seed(1)
+    W = normal(gen, (n, d_in), 0.1, torch.bfloat16).cuda()
+    x = torch.randn(B, d_in, device="cuda").bfloat16()
+    block, layer = GatedLinear(d_in, n, W, W), StructuredLinear(d_in, n, W)
+    h, y = block.forward(x), layer.forward(x, act=B_.ACT_SILU)
+    assert torch.equal(h[-200:], block.forward(x[-200:].contiguous())) and torch.equal(y[-200:], layer.forward(x[-200:].contiguous(), act=B_.ACT_SILU))
+    dx, _, _ = layer.backward(y, x)
+    # (the same order of sums whatever the rows: one part of K in both)
+    want = y[-200:].float() @ W.float()
+    assert (dx[-200:].float() - want).norm() <= (2.0 ** -8 + 1e-5) * want.norm()
+
+
 def test_refused_tensors():
     x, W = torch.zeros(4, 16, device="cuda"), torch.zeros(8, 16, device="cuda")
     block, h = GatedLinear(16, 8, W, W), torch.zeros(4, 8, device="cuda")

@@ -212,6 +212,90 @@ def test_update_takes_the_weight_gradient():
     assert all(torch.equal(a, b) for a, b in zip(*outs)) and outs[0][2][1] > 0
 
 
+@pytest.mark.parametrize("B,d_in,d_out", [(70000, 8, 5), (3, 16, 70001), (300, 40, 30000), (100, 0, 70), (129, 8, 1)])
+@pytest.mark.parametrize("ablated", [0.0, 0.4])
+def test_more_rows_or_neurons_than_a_grid_has_lines(B, d_in, d_out, ablated):
+    gen = torch.Generator().manual_seed(B)
+    W, bias, active, stored = _layer(gen, d_in, d_out, ablated, torch.bfloat16, lambda s, tt: whole(gen, s, 1, tt))
+    x, dy = whole(gen, (B, d_in), 1, torch.bfloat16), whole(gen, (B, d_out), 1, torch.bfloat16)
+    layer = StructuredLinear(d_in, d_out, *_cuda(W, active, bias))
+    want, _, z, _ = linear(x, W, stored, bias, d_out, "relu")
+    y, got_z = layer.forward(x.cuda(), act=B_.ACT_RELU, save=True)
+    assert torch.equal(y.cpu(), want.bfloat16()) and torch.equal(got_z.cpu(), z.bfloat16())
+    dx, dWd, db = layer.backward(dy.cuda(), x.cuda(), got_z, act=B_.ACT_RELU)
+    dz = dy.double()[:, stored] * (got_z.cpu() > 0)
+    dbias = dy.double().sum(0) * (bias > 0)
+    dbias[stored] = dz.sum(0)
+    assert torch.equal(dx.cpu(), (dz @ W.double()).bfloat16()) and torch.equal(dWd.cpu(), (dz.T @ x.double()).bfloat16()) and torch.equal(db.cpu(), dbias.float())
+
+
+@pytest.mark.parametrize("spread", [1, 300, 3000])
+def test_neurons_far_apart(spread):
+    """Stored neurons in runs with long gaps: a workgroup's columns fit its LDS or do not."""
+    gen = torch.Generator().manual_seed(spread)
+    d_out, n = 20000, 700
+    stored = torch.cat([torch.arange(k, k + n // 7) for k in torch.arange(7) * (n // 7 + spread - 1) + 11])
+    active, W, x, bias = stored.int(), whole(gen, (n, 72), 2, torch.bfloat16), whole(gen, (40, 72), 2, torch.bfloat16), whole(gen, (d_out,), 2)
+    dy = whole(gen, (40, d_out), 2, torch.bfloat16)
+    layer = StructuredLinear(72, d_out, *_cuda(W, active, bias))
+    want, _, z, _ = linear(x, W, stored, bias, d_out, "relu")
+    for rows in (40, 5):
+        y, got_z = layer.forward(x[:rows].cuda(), act=B_.ACT_RELU, save=True)
+        assert torch.equal(y.cpu(), want[:rows].bfloat16()) and torch.equal(got_z.cpu(), z[:rows].bfloat16())
+        dx, dWd, db = layer.backward(dy[:rows].cuda(), x[:rows].cuda(), got_z, act=B_.ACT_RELU)
+        dz = dy[:rows].double()[:, stored] * (z[:rows] > 0)
+        dbias = dy[:rows].double().sum(0) * (bias > 0)
+        dbias[stored] = dz.sum(0)
+        assert torch.equal(dx.cpu(), (dz @ W.double()).bfloat16()) and torch.equal(dWd.cpu(), (dz.T @ x[:rows].double()).bfloat16()) and torch.equal(db.cpu(), dbias.float())
+
+
+@pytest.mark.parametrize("B,d_in,d_out", [(3, 264, 100), (100, 264, 300), (70, 137, 90)])
+def test_fp32_from_end_to_end_of_its_range(B, d_in, d_out):
+    """Powers of two from 2^-40 to 2^100: products and sums of one sign keep their relative error, and sums beyond the range are infinite as in fp32."""
+    gen = torch.Generator().manual_seed(4)
+    x, W = torch.rand(B, d_in, generator=gen) + 0.5, torch.rand(d_out, d_in, generator=gen) + 0.5
+    scale = 2.0 ** torch.randint(-40, 100, (B, 1), generator=gen).float()
+    y = StructuredLinear(d_in, d_out, W.cuda()).forward((x * scale).cuda())
+    want = (x * scale).double() @ W.double().T
+    within(y, want, sum_gate(d_in) * want, "y")
+    dx, dWd, _ = StructuredLinear(d_in, d_out, W.cuda()).backward((torch.ones(B, d_out) * scale).cuda(), x.cuda())
+    want = (torch.ones(B, d_out) * scale).double() @ W.double()
+    within(dx, want, sum_gate(d_out) * want, "dx")
+    x[0], W[0] = 3e38, 1.0
+    y = StructuredLinear(d_in, d_out, W.cuda()).forward(x.cuda()).cpu()
+    assert (y[0] == float("inf")).all() and y[1:].isfinite().all()
+    x[0, 1:], W[0, 1:] = 0.0, 0.0
+    y = StructuredLinear(d_in, d_out, W.cuda()).forward(x.cuda()).cpu()
+    assert y[0, 0] == x[0, 0] and y[1:].isfinite().all()
+
+
+def test_same_bits_every_time():
+    gen = torch.Generator().manual_seed(6)
+    for t, B, d_in, d_out in ((torch.float32, 200, 520, 300), (torch.bfloat16, 77, 1001, 400), (torch.bfloat16, 300, 768, 3000)):
+        W, bias, active, stored = _layer(gen, d_in, d_out, 0.2, t, lambda s, tt: normal(gen, s, 0.1, tt))
+        x, dy = normal(gen, (B, d_in), 1.0, t).cuda(), normal(gen, (B, d_out), 1.0, t).cuda()
+        layer, runs = StructuredLinear(d_in, d_out, *_cuda(W, active, bias)), []
+        for _ in range(3):
+            y, z = layer.forward(x, act=B_.ACT_SILU, save=True)
+            runs.append([y, z, *layer.backward(dy, x, z, act=B_.ACT_SILU)])
+        assert all(torch.equal(a, b) for other in runs[1:] for a, b in zip(runs[0], other))
+
+
+def test_condensed_layer_as_dense_rows():
+    """A condensed layer's structured() runs the same layer, with what stands behind the product."""
+    import numpy as np
+    import synth_inputs as si
+    from gpu_util import TOL_F32, dev, gate, host, oracle_condensed
+    from paper_2305_02299_amd import condense_layer
+    import oracle
+    L = si.make_layer(200, 130, 20, 9, ablate_frac=0.3, seed=7)
+    layer = condense_layer(dev(L.W), dev(L.mask), L.K, dev(L.bias)).structured()
+    W_c, idx, active = oracle_condensed(L)
+    y_ref, S = oracle.fwd(L.x, W_c, idx, active, L.bias, 130, want_scale=True)
+    gate(host(layer.forward(dev(L.x))), y_ref, S, TOL_F32)
+    np.testing.assert_array_equal(host(layer.forward(dev(L.x), act=B_.ACT_RELU)), np.maximum(host(layer.forward(dev(L.x))), 0))
+
+
 def test_refused_tensors():
     x, W = torch.zeros(4, 16, device="cuda"), torch.zeros(8, 16, device="cuda")
     layer = StructuredLinear(16, 8, W)
