@@ -898,10 +898,15 @@ __global__ __launch_bounds__(WGM * WGN * 64) void k_dense(P p) {
 
 // Two products that do not wait for each other in one launch (the gradients of x and of W): what one leaves idle the other takes, and a small pass is a launch shorter.  The first one's workgroups come
 // first, then the second one's; both are whole multiples of 8 a part, so that a workgroup's die is the one that tile_of_workgroup expects.
-template <typename T, int BM, int BN, int WGM, int WGN, int NS, class P, class Q>
-__global__ __launch_bounds__(WGM * WGN * 64) void k_dense_two(P p, Q q, int p_wg, int q_wg) {
+// Behind both come the workgroups of something else that waits for neither: more(smem, its workgroup).
+template <typename T, int BM, int BN, int WGM, int WGN, int NS, class P, class Q, class More>
+__global__ __launch_bounds__(WGM * WGN * 64) void k_dense_two(P p, Q q, int p_wg, int q_wg, More more) {
     extern __shared__ __attribute__((aligned(1024))) unsigned char smem[];
     int id = blockIdx.x;
+    if (id >= p_wg * p.parts + q_wg * q.parts) {
+        more(smem, id - (p_wg * p.parts + q_wg * q.parts));
+        return;
+    }
     if (id < p_wg * p.parts) {
         dense_tile<T, BM, BN, WGM, WGN, NS, false>(smem, id % p_wg, id / p_wg, p);
     } else {
@@ -980,15 +985,15 @@ static srigl_status launch_tiles(const DenseProduct<OA, OB, Out>& p, hipStream_t
     }
     return hip_ok(hipGetLastError());
 }
-template <typename T, int BM, int BN, int WGM, int WGN, int NS, class P, class Q>
-static srigl_status launch_tiles_two(const P& p, const Q& q, hipStream_t st) {
+template <typename T, int BM, int BN, int WGM, int WGN, int NS, class P, class Q, class More>
+static srigl_status launch_tiles_two(const P& p, const Q& q, const More& more, hipStream_t st) {
     constexpr size_t lds = dense_lds<BM, BN, WGM, NS, false>();
-    auto kern = k_dense_two<T, BM, BN, WGM, WGN, NS, P, Q>;
+    auto kern = k_dense_two<T, BM, BN, WGM, WGN, NS, P, Q, More>;
     static LdsLimit limit;
     if (limit.ensure(kern, lds) != SRIGL_OK) return SRIGL_ERR_HIP;
-    const long long p_wg = dense_groups<BM, BN>(p), q_wg = dense_groups<BM, BN>(q), all = p_wg * p.parts + q_wg * q.parts;
+    const long long p_wg = dense_groups<BM, BN>(p), q_wg = dense_groups<BM, BN>(q), all = p_wg * p.parts + q_wg * q.parts + more.groups();
     if (all > 0x7fffffffll) return SRIGL_ERR_UNSUPPORTED;
-    hipLaunchKernelGGL(kern, dim3((unsigned)all), dim3(WGM * WGN * 64), lds, st, p, q, (int)p_wg, (int)q_wg);
+    hipLaunchKernelGGL(kern, dim3((unsigned)all), dim3(WGM * WGN * 64), lds, st, p, q, (int)p_wg, (int)q_wg, more);
     const long long pj = join_groups(p, 4), qj = join_groups(q, 4);
     if (pj + qj > 0) hipLaunchKernelGGL((k_dense_join_two<P, Q>), dim3((unsigned)(pj + qj)), dim3(256), 0, st, p, q, (unsigned)pj);
     return hip_ok(hipGetLastError());
@@ -1024,17 +1029,17 @@ static srigl_status launch_dense(const DenseProduct<OA, OB, Out>& p, int tile, h
     return launch_tiles<T, 64, SN, 2, 2, 4, PAIR>(p, st);
 }
 // Both products in tiles of one shape, side by side
-template <typename T, class P, class Q>
-static srigl_status launch_dense_two(const P& p, const Q& q, int tile, hipStream_t st) {
+template <typename T, class P, class Q, class More>
+static srigl_status launch_dense_two(const P& p, const Q& q, const More& more, int tile, hipStream_t st) {
     if (!(p.oa.direct(256) && p.ob.direct(256) && q.oa.direct(256) && q.ob.direct(256))) {
-        if (tile == kTileS) return launch_tiles_two<T, 64, 64, 2, 2, 0>(p, q, st);
-        return launch_tiles_two<T, 128, 128, 2, 2, 0>(p, q, st);
+        if (tile == kTileS) return launch_tiles_two<T, 64, 64, 2, 2, 0>(p, q, more, st);
+        return launch_tiles_two<T, 128, 128, 2, 2, 0>(p, q, more, st);
     }
     if constexpr (sizeof(T) == 2)
-        if (tile == kTileL) return launch_tiles_two<T, 256, 256, 2, 4, 2>(p, q, st);
-    if (tile >= kTileH) return launch_tiles_two<T, 256, 128, 4, 2, 3>(p, q, st);
-    if (tile == kTileM) return launch_tiles_two<T, 128, 128, 2, 2, 4>(p, q, st);
-    return launch_tiles_two<T, 64, 64, 2, 2, 4>(p, q, st);
+        if (tile == kTileL) return launch_tiles_two<T, 256, 256, 2, 4, 2>(p, q, more, st);
+    if (tile >= kTileH) return launch_tiles_two<T, 256, 128, 4, 2, 3>(p, q, more, st);
+    if (tile == kTileM) return launch_tiles_two<T, 128, 128, 2, 2, 4>(p, q, more, st);
+    return launch_tiles_two<T, 64, 64, 2, 2, 4>(p, q, more, st);
 }
 // ---- few rows of x ----
 // Products with at most 64 rows of x are bound by reading the weights.  A workgroup takes 16 neurons (of a pair: of both matrices) and all of K, its wavefronts 128 bytes of the lines in turn, straight

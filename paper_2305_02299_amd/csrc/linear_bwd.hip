@@ -172,28 +172,31 @@ __global__ __launch_bounds__(256) void k_dz_gated(const T* __restrict__ dh, cons
     const int c = (int)((blockIdx.x * (unsigned)kDzCols + threadIdx.x % kDzCols) * V), m0 = blockIdx.y * rows, m1 = min(m0 + rows, B), valid = n - c;
     float sg[V] = {}, su[V] = {};
     if (c < pitch)
-        for (int m = m0 + threadIdx.x / kDzCols; m < m1; m += kDzRows) {
-            float d[V] = {}, gv[V] = {}, uv[V] = {};
-            if (valid > 0) {
-                const size_t at = (size_t)m * n + c;
-                load_values<T, V>(dh + at, d, valid);
-                load_values<T, V>(g + at, gv, valid);
-                load_values<T, V>(u + at, uv, valid);
-                float slope[V];
-                act_slopes<V>(gv, slope, act);
-                act_values<V>(gv, act);
+        for (int base = m0 + threadIdx.x / kDzCols; base < m1; base += 2 * kDzRows) {   // (two rows' loads together)
+            float d[2][V] = {}, gv[2][V] = {}, uv[2][V] = {}, slope[V];
+#pragma unroll
+            for (int r = 0; r < 2; ++r)
+                if (valid > 0 && base + r * kDzRows < m1) {
+                    const size_t at = (size_t)(base + r * kDzRows) * n + c;
+                    load_values<T, V>(dh + at, d[r], valid);
+                    load_values<T, V>(g + at, gv[r], valid);
+                    load_values<T, V>(u + at, uv[r], valid);
+                }
+#pragma unroll
+            for (int r = 0; r < 2; ++r) {
+                if (base + r * kDzRows >= m1) break;
+                act_slopes<V>(gv[r], slope, act);
+                act_values<V>(gv[r], act);
 #pragma unroll
                 for (int q = 0; q < V; ++q) {
-                    const float dg = d[q] * uv[q] * slope[q], du = d[q] * gv[q];
-                    gv[q] = q < valid ? dg : 0.0f;
-                    uv[q] = q < valid ? du : 0.0f;
-                    sg[q] += gv[q];
-                    su[q] += uv[q];
+                    const float dg = d[r][q] * uv[r][q] * slope[q], du = d[r][q] * gv[r][q];
+                    sg[q] += gv[r][q] = q < valid ? dg : 0.0f;
+                    su[q] += uv[r][q] = q < valid ? du : 0.0f;
                 }
+                T* const to = dz + (size_t)(base + r * kDzRows) * 2 * pitch + c;
+                store_values<T, V>(to, gv[r], V);
+                store_values<T, V>(to + pitch, uv[r], V);
             }
-            T* const to = dz + (size_t)m * 2 * pitch + c;
-            store_values<T, V>(to, gv, V);
-            store_values<T, V>(to + pitch, uv, V);
         }
     if (!sums) return;
     sum_row_lanes<V>(held, sg);
@@ -205,26 +208,39 @@ __global__ __launch_bounds__(256) void k_dz_gated(const T* __restrict__ dh, cons
     }
 }
 
-// Bias gradients from the chunks' sums: four lanes take every fourth chunk of a column each.  Columns [0, n) to first, [n, 2 n) to second (a layer: all to first, ablated
+// Bias gradients from the chunks' sums, 64 columns to a workgroup, whose wavefronts take chunks by turns.  Columns [0, n) to first, [n, 2 n) to second (a layer: all to first, ablated
 // columns times the slope at their bias).
-__global__ __launch_bounds__(256) void k_sum_chunks(const float* __restrict__ sums, int chunks, int cols, int n, const int32_t* __restrict__ active, int n_active,
-                                                   const float* __restrict__ bias, int act, float* __restrict__ first, float* __restrict__ second) {
-    __shared__ float held[4][64];
-    const int c = blockIdx.x * 64 + (threadIdx.x & 63), lane = threadIdx.x >> 6;
-    float v = 0.0f;
-    if (c < cols)
+struct SumChunks {
+    const float* sums;
+    int chunks, cols, n;
+    const int32_t* active;
+    int n_active;
+    const float* bias;
+    int act;
+    float *first, *second;
+    long long groups() const { return first || second ? (cols + 63ll) / 64 : 0; }
+    __device__ __forceinline__ void operator()(unsigned char* smem, int group) const {
+        float(*const held)[64] = reinterpret_cast<float(*)[64]>(smem);
+        const int c = group * 64 + (threadIdx.x & 63), wave = threadIdx.x >> 6, waves = blockDim.x >> 6;
+        float v = 0.0f;
+        if (c < cols)
 #pragma unroll 8
-        for (int k = lane; k < chunks; k += 4) v += sums[(size_t)k * cols + c];
-    held[lane][threadIdx.x & 63] = v;
-    __syncthreads();
-    if (lane != 0 || c >= cols) return;
-    v = (held[0][c & 63] + held[1][c & 63]) + (held[2][c & 63] + held[3][c & 63]);
-    if (n_active < n) {
-        const int s = n_active ? place_of(active, n_active, c) : 0;
-        if (!(s < n_active && active[s] == c)) v *= act_slope(bias ? bias[c] : 0.0f, act);
+            for (int k = wave; k < chunks; k += waves) v += sums[(size_t)k * cols + c];
+        held[wave][threadIdx.x & 63] = v;
+        __syncthreads();
+        if (wave != 0 || c >= cols) return;
+        for (int w = 1; w < waves; ++w) v += held[w][c & 63];
+        if (n_active < n) {
+            const int s = n_active ? place_of(active, n_active, c) : 0;
+            if (!(s < n_active && active[s] == c)) v *= act_slope(bias ? bias[c] : 0.0f, act);
+        }
+        float* const to = c < n ? first : second;
+        if (to) to[c < n ? c : c - n] = v;
     }
-    float* const to = c < n ? first : second;
-    if (to) to[c < n ? c : c - n] = v;
+};
+__global__ __launch_bounds__(256) void k_sum_chunks(SumChunks s) {
+    __shared__ unsigned char held[4 * 64 * sizeof(float)];
+    s(held, blockIdx.x);
 }
 
 template <typename T>
@@ -278,8 +294,10 @@ static BwdPlan plan_bwd(int B, int d_in, long long cols, long long K, long long 
 }
 
 template <typename T, class P, class Q>
-static srigl_status launch_gradients(const DensePlans& plans, const P& of_x, bool want_x, const Q& of_W, bool want_W, hipStream_t st) {
-    if (want_x && want_W && plans.together && of_x.M > 0 && of_W.M > 0) return launch_dense_two<T>(of_x, of_W, plans.dx.tile, st);
+static srigl_status launch_gradients(const DensePlans& plans, const P& of_x, bool want_x, const Q& of_W, bool want_W, const SumChunks& sums, hipStream_t st) {
+    if (want_x && want_W && plans.together && of_x.M > 0 && of_W.M > 0) return launch_dense_two<T>(of_x, of_W, sums, plans.dx.tile, st);
+    if (sums.groups() > 0) hipLaunchKernelGGL(k_sum_chunks, dim3((unsigned)sums.groups()), dim3(256), 0, st, sums);
+    if (hip_ok(hipGetLastError()) != SRIGL_OK) return SRIGL_ERR_HIP;
     const srigl_status rc = want_x ? launch_dense<T, false>(of_x, plans.dx.tile, st) : SRIGL_OK;
     return rc == SRIGL_OK && want_W ? launch_dense<T, false>(of_W, plans.dW.tile, st) : rc;
 }
@@ -304,13 +322,12 @@ static srigl_status linear_bwd(const BwdPlan& p, const void* dy, const void* x, 
             hipLaunchKernelGGL((k_dz_linear<T, TY>), dim3((unsigned)((pitch + COLS - 1) / COLS), (unsigned)p.chunks), dim3(256), 0, st, (const TY*)dy, (const T*)z, n, B, act, to, pitch, sum_to,
                                p.chunk_rows);
     }
-    if (dbias) hipLaunchKernelGGL(k_sum_chunks, dim3((unsigned)((d_out + 63ll) / 64)), dim3(256), 0, st, sums, p.chunks, d_out, d_out, active, n, bias, act, dbias, nullptr);
     const T* const d = as_it_is ? (const T*)dy : dz;
     const int d_pitch = as_it_is ? n : pitch;
     if (hip_ok(hipGetLastError()) != SRIGL_OK) return SRIGL_ERR_HIP;
     const DenseProduct<RowsOf<T>, ColsOf<T>, PlainOut<T>> of_x{{d, d_pitch, B - 1, d_pitch}, {(const T*)Wd, d_in, d_in, n}, {(T*)dx, d_in}, B, d_in, stages_of<T>(n), p.products.dx.parts, dx_part};
     const DenseProduct<ColsOf<T>, ColsOf<T>, PlainOut<T>> of_W{{d, d_pitch, d_pitch, B}, {(const T*)x, d_in, d_in, B}, {(T*)dWd, d_in}, n, d_in, stages_of<T>(B), p.products.dW.parts, dW_part};
-    return launch_gradients<T>(p.products, of_x, dx != nullptr, of_W, dWd != nullptr, st);
+    return launch_gradients<T>(p.products, of_x, dx != nullptr, of_W, dWd != nullptr, SumChunks{sums, p.chunks, d_out, d_out, active, n, bias, act, dbias, nullptr}, st);
 }
 
 template <typename T>
@@ -323,14 +340,12 @@ static srigl_status gated_bwd(const BwdPlan& p, const void* dh, const void* x, i
     if (p.chunks > 0 && n > 0)
         hipLaunchKernelGGL(k_dz_gated<T>, dim3((unsigned)((pitch + kDzCols * kPiece<T> - 1) / (kDzCols * kPiece<T>)), (unsigned)p.chunks), dim3(256), 0, st, (const T*)dh, (const T*)g, (const T*)u, n, B, act, dz,
                            pitch, want_sums ? sums : nullptr, p.chunk_rows);
-    if (want_sums && n > 0)
-        hipLaunchKernelGGL(k_sum_chunks, dim3((unsigned)((2ll * n + 63) / 64)), dim3(256), 0, st, sums, p.chunks, 2 * n, n, nullptr, n, nullptr, act, dbias_g, dbias_u);
     if (hip_ok(hipGetLastError()) != SRIGL_OK) return SRIGL_ERR_HIP;
     const DenseProduct<RowsOf<T>, PairedCols<T>, PlainOut<T>> of_x{{dz, 2ll * pitch, B - 1, 2 * pitch}, {(const T*)Wg, bytes_between(Wg, Wu), d_in, d_in, n, pitch}, {(T*)dx, d_in}, B, d_in,
                                                                   stages_of<T>(2ll * pitch), p.products.dx.parts, dx_part};
     const DenseProduct<ColsOf<T>, ColsOf<T>, TwoOut<T>> of_W{{dz, 2ll * pitch, 2 * pitch, B}, {(const T*)x, d_in, d_in, B}, {(T*)dWg, (T*)dWu, d_in, n, pitch}, 2 * pitch, d_in, stages_of<T>(B),
                                                             p.products.dW.parts, dW_part};
-    return launch_gradients<T>(p.products, of_x, dx != nullptr, of_W, dWg || dWu, st);
+    return launch_gradients<T>(p.products, of_x, dx != nullptr, of_W, dWg || dWu, SumChunks{sums, p.chunks, 2 * n, n, nullptr, n, nullptr, act, dbias_g, dbias_u}, st);
 }
 
 static bool bwd_sizes_fit(int B, int d_in, int d_out) { return B <= kMaxSide && d_in <= kMaxSide && d_out <= kMaxSide / 2; }
