@@ -390,16 +390,16 @@ struct DirectStage {
     }
 };
 
-// Whole stages h0 .. h1 - 1, by their number.  (The part of a stage behind the end of K in the loop, its pieces from zeros by lane: 20 % longer in 128 x 128 tiles.)
-template <typename T, int BM, int BN, int WGM, int WGN, int NS, class OA, class OB>
-__device__ __forceinline__ void direct_product_of_tile(unsigned char* smem, const OA& oa, const OB& ob, int h0, int h1, f32x16_t (&acc)[BM / WGM / 32][BN / WGN / 32]) {
+// Whole stages h0 .. h1 - 1, by their number; meanwhile(): done while the first ones are on their way.  (The part of a stage behind the end of K in the loop, its pieces from zeros by lane: 20 % longer in 128 x 128 tiles.)
+template <typename T, int BM, int BN, int WGM, int WGN, int NS, class OA, class OB, class Meanwhile>
+__device__ __forceinline__ void direct_product_of_tile(unsigned char* smem, const OA& oa, const OB& ob, int h0, int h1, f32x16_t (&acc)[BM / WGM / 32][BN / WGN / 32], Meanwhile meanwhile) {
     constexpr int NWAVES = WGM * WGN, TM = BM / WGM / 32, TN = BN / WGN / 32, KSTEPS = kLineBytes / 32, STAGE = (BM + BN) * kLineBytes;
     using SA = DirectStage<T, BM, 0, NWAVES, OA>;
     using SB = DirectStage<T, BN, BM * kLineBytes, NWAVES, OB>;
     constexpr int PASSES = SA::PASSES + SB::PASSES;
     static_assert(NS >= 2 && (NS - 1) * PASSES <= 63, "vmcnt range");
     const int lane = threadIdx.x & 63, wv = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), wm = wv / WGN, wn = wv % WGN, n_st = h1 - h0;
-    if (n_st <= 0) return;
+    if (n_st <= 0) return meanwhile();
     SA la;
     SB lb;
     la.init(oa, wv, lane);
@@ -414,6 +414,7 @@ __device__ __forceinline__ void direct_product_of_tile(unsigned char* smem, cons
     for (int s = 0; s < NS; ++s)
 #pragma unroll
         for (int p = 0; p < (s < NS - 1 ? PASSES : EARLY); ++p) issue_piece(p, s, s * STAGE);
+    meanwhile();
 
     FragReader<T, OA::kAlong, BM, TM> fa;
     FragReader<T, OB::kAlong, BN, TN> fb;
@@ -474,8 +475,8 @@ __device__ __forceinline__ void direct_product_of_tile(unsigned char* smem, cons
 }
 
 // Whole stages h0 .. h1 - 1 of an fp32 product by direct loads, as in direct_product_of_tile: two steps of 16 k a stage
-template <int BM, int BN, int WGM, int WGN, int NS, class OA, class OB>
-__device__ __forceinline__ void split_product_of_tile(unsigned char* smem, const OA& oa, const OB& ob, int h0, int h1, f32x16_t (&acc)[BM / WGM / 32][BN / WGN / 32]) {
+template <int BM, int BN, int WGM, int WGN, int NS, class OA, class OB, class Meanwhile>
+__device__ __forceinline__ void split_product_of_tile(unsigned char* smem, const OA& oa, const OB& ob, int h0, int h1, f32x16_t (&acc)[BM / WGM / 32][BN / WGN / 32], Meanwhile meanwhile) {
     constexpr int NWAVES = WGM * WGN, TM = BM / WGM / 32, TN = BN / WGN / 32, KSTEPS = 2, STAGE = (BM + BN) * kLineBytes;
     using SA = DirectStage<float, BM, 0, NWAVES, OA>;
     using SB = DirectStage<float, BN, BM * kLineBytes, NWAVES, OB>;
@@ -483,7 +484,7 @@ __device__ __forceinline__ void split_product_of_tile(unsigned char* smem, const
     constexpr int N_FRAG = TM + TN, N_BLOCK = TM * TN, N_MMA = 6 * N_BLOCK, N_PAIR = 4 * N_FRAG, WAIT = N_MMA / 4 + 1;   // the cutting begins behind so many multiplications
     static_assert(NS >= 2 && (NS - 1) * PASSES <= 63, "vmcnt range");
     const int lane = threadIdx.x & 63, wv = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), wm = wv / WGN, wn = wv % WGN, n_st = h1 - h0;
-    if (n_st <= 0) return;
+    if (n_st <= 0) return meanwhile();
     SA la;
     SB lb;
     la.init(oa, wv, lane);
@@ -497,6 +498,7 @@ __device__ __forceinline__ void split_product_of_tile(unsigned char* smem, const
     for (int s = 0; s < NS; ++s)
 #pragma unroll
         for (int p = 0; p < (s < NS - 1 ? PASSES : EARLY); ++p) issue_piece(p, s, s * STAGE);
+    meanwhile();
     SplitReader<OA::kAlong, BM, TM> fa;
     SplitReader<OB::kAlong, BN, TN> fb;
     fa.init(wm * TM, lane);
@@ -622,19 +624,24 @@ __device__ __forceinline__ void pair_as_rows(unsigned char* smem, const f32x16_t
 // last neuron are one range, which passes through the LDS in windows of EL::COLS at its final columns.  out.listed(m, c, first, valid, v, gaps, flat): V columns from c on, of
 // which [first, valid) are this tile's; columns with their bit in gaps are ablated and are `flat`.  out.stored(m, s, valid, v): sums (with bias) of neurons s .. in their own
 // order, where out.wants_stored().
+template <int BN, int V, class Out>
+__device__ __forceinline__ TileColumns listed_columns(int n0, const Out& out) {
+    TileColumns cols = tile_columns(n0, BN, out.active, out.n_active, out.d_out, 0);
+    cols.base = cols.lo / V * V;   // (16-byte stores begin at whole pieces of the row)
+    return cols;
+}
+// (tables: of the first window, filled)
 template <int BM, int BN, int WGM, int WGN, int V, class Out>
-__device__ __forceinline__ void listed_as_rows(unsigned char* smem, const f32x16_t (&acc)[BM / WGM / 32][BN / WGN / 32], int m0, int n0, int M, Out& out) {
+__device__ __forceinline__ void listed_as_rows(unsigned char* smem, unsigned char* tables, const f32x16_t (&acc)[BM / WGM / 32][BN / WGN / 32], int m0, int n0, int M, Out& out) {
     using EL = EpiLayout<BN, WGM>;
     constexpr int NT = WGM * WGN * 64, TM = BM / WGM / 32, TN = BN / WGN / 32, PITCH = EL::PITCH, GROUPS = EL::COLS / V, STEP = NT / GROUPS;
     static_assert(NT % GROUPS == 0 && EL::COLS >= BN, "a thread keeps its columns");
     float* const tile = reinterpret_cast<float*>(smem);
-    unsigned char* const tables = smem + EL::TILE_BYTES;
     const int* const place = reinterpret_cast<const int*>(tables);
     const int* const table = place + BN;
     float* const tbias = reinterpret_cast<float*>(tables + (size_t)(BN + EL::COLS) * 4);
     const int tid = threadIdx.x, lane = tid & 63, wv = __builtin_amdgcn_readfirstlane(tid >> 6), wm = wv / WGN, wn = wv % WGN;
-    TileColumns cols = tile_columns(n0, BN, out.active, out.n_active, out.d_out, 0);
-    cols.base = cols.lo / V * V;   // (16-byte stores begin at whole pieces of the row)
+    const TileColumns cols = listed_columns<BN, V>(n0, out);
     if (out.wants_stored()) {
         const int c = (tid % (BN / V)) * V, valid = cols.stored - c;
         if (valid > 0) out.template start<V>(n0 + c, valid);
@@ -655,8 +662,10 @@ __device__ __forceinline__ void listed_as_rows(unsigned char* smem, const f32x16
     }
     for (int cc = cols.base; cc <= cols.hi; cc += EL::COLS) {
         const int wc = min(EL::COLS, cols.hi - cc + 1), head = max(cols.lo - cc, 0);
-        if (cc != cols.base) __syncthreads();   // the window before is done with the tables
-        fill_table<BN, WGM, NT>(tables, cc, cols, n0, out.active, out.bias);
+        if (cc != cols.base) {
+            __syncthreads();   // the window before is done with the tables
+            fill_table<BN, WGM, NT>(tables, cc, cols, n0, out.active, out.bias);
+        }
         __syncthreads();
         int at[TN];   // this lane's columns in the window
         float add[TN];
@@ -839,6 +848,11 @@ struct DenseProduct {
     float* part;
 };
 
+template <int BM, int BN, int WGM, int NS, bool LISTED>
+constexpr size_t dense_lds() {
+    const size_t ring = (size_t)(NS > 0 ? NS : 1) * (BM + BN) * kLineBytes, rows = LISTED ? EpiLayout<BN, WGM>::TILE_BYTES : rows_lds<BM, BN, WGM>();
+    return (ring > rows ? ring : rows) + (LISTED ? EpiLayout<BN, WGM>::TABLE_BYTES : 0);
+}
 // Tile `id` (of tile_of_workgroup's order) and part `part_no` of a product.  NS: stages of the ring of direct loads, 0: staged through registers.
 template <typename T, int BM, int BN, int WGM, int WGN, int NS, bool PAIR, class OA, class OB, class Out>
 __device__ __forceinline__ void dense_tile(unsigned char* smem, int id, int part_no, DenseProduct<OA, OB, Out>& p) {
@@ -861,9 +875,23 @@ __device__ __forceinline__ void dense_tile(unsigned char* smem, int id, int part
     };
     clear();
     constexpr bool SPLIT = sizeof(T) == 4;
-    if constexpr (NS == 0) product_of_tile<T, SPLIT, BM, BN, WGM, WGN>(smem, p.oa, p.ob, h0, h1, acc);
-    else if constexpr (SPLIT) split_product_of_tile<BM, BN, WGM, WGN, NS>(smem, p.oa, p.ob, h0, h1, acc);
-    else direct_product_of_tile<T, BM, BN, WGM, WGN, NS>(smem, p.oa, p.ob, h0, h1, acc);
+    // (a list's tables stand behind everything else in the LDS, filled while the first stages come: two waits for memory that a small product would end with)
+    unsigned char* const tables = smem + dense_lds<BM, BN, WGM, NS, Out::kListed>() - (Out::kListed ? EpiLayout<BN, WGM>::TABLE_BYTES : 0);
+    const auto meanwhile = [&] {
+        if constexpr (Out::kListed)
+            if (p.out.active && parts == 1) {
+                const TileColumns cols = listed_columns<BN, V>(n0, p.out);
+                fill_table<BN, WGM, WGM * WGN * 64>(tables, cols.base, cols, n0, p.out.active, p.out.bias);
+            }
+    };
+    if constexpr (NS == 0) {
+        meanwhile();
+        product_of_tile<T, SPLIT, BM, BN, WGM, WGN>(smem, p.oa, p.ob, h0, h1, acc);
+    } else if constexpr (SPLIT) {
+        split_product_of_tile<BM, BN, WGM, WGN, NS>(smem, p.oa, p.ob, h0, h1, acc, meanwhile);
+    } else {
+        direct_product_of_tile<T, BM, BN, WGM, WGN, NS>(smem, p.oa, p.ob, h0, h1, acc, meanwhile);
+    }
     if constexpr (SPLIT)
         if (not_finite<WGM * WGN>(smem, acc)) {
             clear();
@@ -883,7 +911,7 @@ __device__ __forceinline__ void dense_tile(unsigned char* smem, int id, int part
     }
     if constexpr (Out::kListed)
         if (p.out.active) {
-            listed_as_rows<BM, BN, WGM, WGN, V>(smem, acc, m0, n0, p.M, p.out);
+            listed_as_rows<BM, BN, WGM, WGN, V>(smem, tables, acc, m0, n0, p.M, p.out);
             return;
         }
     if constexpr (PAIR) pair_as_rows<BM, BN, WGM, WGN, V>(smem, acc, m0, n0, p.M, p.N, p.out);
@@ -954,11 +982,6 @@ __global__ __launch_bounds__(256) void k_dense_join_two(P p, Q q, unsigned p_gro
 // workgroups of a join
 template <class P> inline long long join_groups(const P& p, int V) { return p.parts > 1 ? ((long long)p.M * ((p.N + V - 1ll) / V) + 255) / 256 : 0; }
 
-template <int BM, int BN, int WGM, int NS, bool LISTED>
-constexpr size_t dense_lds() {
-    const size_t ring = (size_t)(NS > 0 ? NS : 1) * (BM + BN) * kLineBytes, rows = LISTED ? EpiLayout<BN, WGM>::BYTES : rows_lds<BM, BN, WGM>();
-    return ring > rows ? ring : rows;
-}
 // workgroups of a part
 template <int BM, int COLS, class P> inline long long dense_groups(const P& p) {
     return (((p.M + BM - 1ll) / BM) * ((p.N + COLS - 1ll) / COLS) + kXcds - 1) / kXcds * kXcds;
@@ -1001,7 +1024,8 @@ static srigl_status launch_tiles_two(const P& p, const Q& q, const More& more, h
 
 // Tile and parts of K of a product (of a pair: N neurons, two sums each)
 struct DensePlan { int tile, parts; };
-enum { kTileS = 0, kTileM = 1, kTileH = 2, kTileL = 3 };   // 64 x 64 (of a pair 64 x 128), 128 x 128, 256 x 128 (direct loads) and 256 x 256 (and bf16)
+enum { kTileS = 0, kTileM = 1, kTileH = 2, kTileL = 3, kTileS2 = 4, kTileM2 = 5 };   // 64 x 64 (of a pair 64 x 128), 128 x 128, 256 x 128 (direct loads) and 256 x 256 (and bf16)
+// S2, M2: S and M with two stages of the ring in place of four, so that five and two workgroups share a compute unit: one stores while another loads, for short K and large results
 enum DenseKind { kDenseForward = 0, kDensePair = 1, kDenseGradX = 2, kDenseGradW = 3 };   // a layer's forward product, a gated block's, gradients of x and of W
 // direct: rows are multiples of 16 bytes (a choice by sizes, so that the workspace does not depend on addresses)
 DensePlan plan_dense(DenseKind kind, int M, int N, int stages, bool f32, bool direct);
@@ -1021,11 +1045,13 @@ static srigl_status launch_dense(const DenseProduct<OA, OB, Out>& p, int tile, h
     }
     if constexpr (sizeof(T) == 2)
         if (tile == kTileL) return launch_tiles<T, 256, 256, 2, 4, 2, PAIR>(p, st);
-    if (tile >= kTileH) return launch_tiles<T, 256, 128, 4, 2, 3, PAIR>(p, st);
+    if (tile == kTileH || tile == kTileL) return launch_tiles<T, 256, 128, 4, 2, 3, PAIR>(p, st);
     // 128 x 128 by eight wavefronts where both operands' lines run along K, in bf16 (four of 64 x 64 leave each SIMD one, which waits at every barrier: 512 rows, 768 -> 3072, 15.2 us, now 11.5); the
     // transposing reads of half as wide wavefronts are 1.5 times as many (gradient of W, 2048 rows, 4096 -> 4096, 83.5 us against 77.8), and so is the cutting of fp32 (forward, 409 and 364)
     constexpr bool EIGHT = sizeof(T) == 2 && OA::kAlong && OB::kAlong;
     if (tile == kTileM) return launch_tiles<T, 128, 128, EIGHT && PAIR ? 4 : 2, EIGHT && !PAIR ? 4 : 2, 4, PAIR>(p, st);
+    if (tile == kTileM2) return launch_tiles<T, 128, 128, EIGHT && PAIR ? 4 : 2, EIGHT && !PAIR ? 4 : 2, 2, PAIR>(p, st);
+    if (tile == kTileS2) return launch_tiles<T, 64, SN, 2, 2, 2, PAIR>(p, st);
     return launch_tiles<T, 64, SN, 2, 2, 4, PAIR>(p, st);
 }
 // Both products in tiles of one shape, side by side
@@ -1037,8 +1063,10 @@ static srigl_status launch_dense_two(const P& p, const Q& q, const More& more, i
     }
     if constexpr (sizeof(T) == 2)
         if (tile == kTileL) return launch_tiles_two<T, 256, 256, 2, 4, 2>(p, q, more, st);
-    if (tile >= kTileH) return launch_tiles_two<T, 256, 128, 4, 2, 3>(p, q, more, st);
+    if (tile == kTileH || tile == kTileL) return launch_tiles_two<T, 256, 128, 4, 2, 3>(p, q, more, st);
     if (tile == kTileM) return launch_tiles_two<T, 128, 128, 2, 2, 4>(p, q, more, st);
+    if (tile == kTileM2) return launch_tiles_two<T, 128, 128, 2, 2, 2>(p, q, more, st);
+    if (tile == kTileS2) return launch_tiles_two<T, 64, 64, 2, 2, 2>(p, q, more, st);
     return launch_tiles_two<T, 64, 64, 2, 2, 4>(p, q, more, st);
 }
 // ---- few rows of x ----

@@ -10,8 +10,8 @@ namespace srigl {
 
 // Expected time (us) of a product in a tile and `parts` parts of K: a fixed part, a part a round of workgroups over the compute units and, by 1000 elements of K, a part a round and one that follows how
 // full the rounds are, a part per million results, a second launch and the parts' sums (a million of them written and read) where there are several.  Non-negative least squares on the relative error of
-// 180000 timings in graphs, every tile and 1 to 16 parts of 30000 random products (17 to 2048 rows, 100 to 4096 wide, 100 to 16384 neurons): 4 to 10 % a timing; the tile and parts of smallest time are 0.1
-// to 1.3 % behind the fastest on average by kind and type, 8 % at worst in 95 of 100, 37 % at worst.
+// 145000 timings in graphs, every tile and 1 to 16 parts of 26000 random products (17 to 2048 rows, 100 to 4096 wide, 100 to 16384 neurons): 4 to 10 % a timing; the tile and parts of smallest time are 0.3
+// to 2 % behind the fastest on average by kind and type, 9 % at worst in 95 of 100, 34 % at worst.
 struct DenseModel {
     int kind, f32, direct, tile, slots;
     float us[7];   // fixed, round, per_k, per_k_full, results, second, part
@@ -19,48 +19,64 @@ struct DenseModel {
 static const DenseModel kDenseModels[] = {
     {0, 0, 0, 0, 512, {4.47f, 1.49f, 6.49f, 4.98f, 0.904f, 2.48f, 1.67f}},
     {0, 0, 0, 1, 512, {10.8f, 0.0f, 12.6f, 9.99f, 0.63f, 1.49f, 1.5f}},
-    {0, 0, 1, 0, 512, {3.49f, 2.7f, 2.91f, 4.71f, 0.509f, 2.0f, 2.48f}},
-    {0, 0, 1, 1, 256, {4.8f, 3.06f, 5.67f, 4.17f, 0.502f, 2.24f, 1.63f}},
-    {0, 0, 1, 2, 256, {7.47f, 2.08f, 8.42f, 5.26f, 0.699f, 2.13f, 1.48f}},
-    {0, 0, 1, 3, 256, {10.5f, 3.56f, 15.1f, 9.99f, 0.505f, 1.13f, 1.14f}},
+    {0, 0, 1, 0, 512, {3.45f, 2.42f, 2.78f, 4.74f, 0.441f, 2.52f, 2.29f}},
+    {0, 0, 1, 1, 256, {4.08f, 2.88f, 5.65f, 4.3f, 0.355f, 3.02f, 1.66f}},
+    {0, 0, 1, 2, 256, {6.23f, 2.42f, 8.37f, 5.95f, 0.473f, 3.16f, 1.48f}},
+    {0, 0, 1, 3, 256, {7.88f, 4.07f, 15.1f, 10.5f, 0.285f, 3.67f, 1.16f}},
+    {0, 0, 1, 4, 512, {3.38f, 2.13f, 3.06f, 5.78f, 0.207f, 2.82f, 1.73f}},
+    {0, 0, 1, 5, 512, {6.44f, 0.0f, 5.73f, 14.0f, 0.331f, 3.25f, 1.49f}},
     {0, 1, 0, 0, 512, {5.57f, 0.363f, 19.8f, 13.9f, 1.26f, 2.37f, 1.98f}},
     {0, 1, 0, 1, 512, {10.9f, 0.0f, 49.0f, 32.5f, 0.884f, 0.751f, 1.53f}},
-    {0, 1, 1, 0, 256, {6.61f, 0.0f, 15.5f, 0.0f, 1.55f, 2.72f, 1.87f}},
-    {0, 1, 1, 1, 256, {8.27f, 4.51f, 31.1f, 10.7f, 1.28f, 1.27f, 1.61f}},
-    {0, 1, 1, 2, 256, {10.2f, 3.03f, 56.5f, 17.2f, 0.884f, 2.43f, 1.5f}},
+    {0, 1, 1, 0, 256, {6.46f, 0.0f, 15.3f, 0.0f, 1.42f, 2.9f, 1.86f}},
+    {0, 1, 1, 1, 256, {7.6f, 4.37f, 31.1f, 10.6f, 1.09f, 2.11f, 1.65f}},
+    {0, 1, 1, 2, 256, {10.3f, 2.36f, 56.2f, 17.2f, 0.719f, 3.11f, 1.49f}},
+    {0, 1, 1, 4, 512, {4.87f, 0.696f, 17.7f, 14.6f, 1.06f, 3.08f, 2.12f}},
+    {0, 1, 1, 5, 256, {11.3f, 0.0f, 35.1f, 7.87f, 0.607f, 2.8f, 1.23f}},
     {1, 0, 0, 0, 1024, {7.51f, 0.0f, 9.0f, 21.7f, 0.416f, 2.47f, 1.7f}},
     {1, 0, 0, 1, 512, {10.4f, 0.0f, 12.5f, 10.0f, 0.361f, 2.25f, 1.3f}},
-    {1, 0, 1, 0, 256, {3.6f, 3.77f, 4.39f, 2.74f, 0.488f, 2.62f, 1.53f}},
-    {1, 0, 1, 1, 256, {4.13f, 3.35f, 5.59f, 4.26f, 0.343f, 2.83f, 1.63f}},
-    {1, 0, 1, 2, 256, {6.5f, 2.58f, 8.5f, 4.94f, 0.55f, 2.73f, 1.46f}},
-    {1, 0, 1, 3, 256, {9.16f, 3.71f, 15.3f, 9.14f, 0.348f, 2.44f, 1.12f}},
+    {1, 0, 1, 0, 256, {3.24f, 3.56f, 4.42f, 2.4f, 0.422f, 3.2f, 1.65f}},
+    {1, 0, 1, 1, 256, {3.63f, 3.11f, 5.8f, 3.86f, 0.285f, 3.48f, 1.7f}},
+    {1, 0, 1, 2, 256, {5.45f, 2.68f, 8.6f, 4.99f, 0.452f, 3.95f, 1.51f}},
+    {1, 0, 1, 3, 256, {7.49f, 3.56f, 15.6f, 8.22f, 0.328f, 4.39f, 1.16f}},
+    {1, 0, 1, 4, 1280, {4.34f, 1.72f, 4.83f, 25.8f, 0.394f, 3.38f, 1.86f}},
+    {1, 0, 1, 5, 512, {6.0f, 0.0f, 6.05f, 13.1f, 0.359f, 4.03f, 1.5f}},
     {1, 1, 0, 0, 768, {6.89f, 0.0f, 29.4f, 44.4f, 0.719f, 3.07f, 1.73f}},
     {1, 1, 0, 1, 512, {9.19f, 0.0f, 48.5f, 36.9f, 0.664f, 2.69f, 1.42f}},
-    {1, 1, 1, 0, 256, {3.68f, 4.28f, 22.4f, 6.52f, 0.75f, 3.52f, 1.48f}},
-    {1, 1, 1, 1, 256, {6.43f, 4.67f, 31.6f, 10.7f, 0.962f, 3.2f, 1.54f}},
-    {1, 1, 1, 2, 256, {8.04f, 3.38f, 56.6f, 18.0f, 0.745f, 4.64f, 1.38f}},
+    {1, 1, 1, 0, 256, {3.59f, 3.85f, 22.5f, 6.51f, 0.74f, 3.73f, 1.73f}},
+    {1, 1, 1, 1, 256, {6.02f, 4.16f, 31.8f, 10.1f, 0.89f, 3.78f, 1.76f}},
+    {1, 1, 1, 2, 256, {7.95f, 2.77f, 56.8f, 17.0f, 0.724f, 5.03f, 1.52f}},
+    {1, 1, 1, 4, 1280, {5.49f, 0.747f, 24.5f, 81.3f, 0.973f, 3.91f, 1.97f}},
+    {1, 1, 1, 5, 256, {9.44f, 0.0f, 37.4f, 5.78f, 0.584f, 4.65f, 1.25f}},
     {2, 0, 0, 0, 1536, {5.67f, 0.0f, 11.0f, 13.7f, 0.375f, 2.93f, 2.48f}},
     {2, 0, 0, 1, 1536, {8.5f, 0.0f, 16.4f, 30.0f, 0.123f, 3.27f, 1.67f}},
-    {2, 0, 1, 0, 256, {7.2f, 0.119f, 3.6f, 1.06f, 0.503f, 2.87f, 2.85f}},
-    {2, 0, 1, 1, 256, {7.95f, 1.58f, 5.67f, 3.77f, 0.394f, 3.38f, 2.38f}},
-    {2, 0, 1, 2, 256, {9.2f, 0.299f, 8.67f, 4.92f, 0.479f, 3.87f, 1.88f}},
-    {2, 0, 1, 3, 256, {10.8f, 0.656f, 15.9f, 8.48f, 0.602f, 4.97f, 1.46f}},
+    {2, 0, 1, 0, 256, {7.24f, 0.111f, 3.43f, 1.18f, 0.444f, 2.95f, 2.83f}},
+    {2, 0, 1, 1, 256, {7.74f, 1.77f, 5.71f, 3.68f, 0.271f, 3.56f, 2.31f}},
+    {2, 0, 1, 2, 256, {9.01f, 0.524f, 8.63f, 5.41f, 0.424f, 4.03f, 1.84f}},
+    {2, 0, 1, 3, 256, {10.2f, 1.13f, 15.7f, 9.17f, 0.573f, 5.14f, 1.41f}},
+    {2, 0, 1, 4, 1024, {6.36f, 0.0f, 5.98f, 8.31f, 0.525f, 3.16f, 2.84f}},
+    {2, 0, 1, 5, 1280, {8.36f, 0.0f, 8.42f, 29.2f, 0.0758f, 3.71f, 1.83f}},
     {2, 1, 0, 0, 1536, {2.33f, 3.37f, 29.8f, 48.8f, 0.708f, 3.16f, 2.76f}},
     {2, 1, 0, 1, 512, {8.58f, 0.0f, 62.7f, 29.3f, 0.431f, 3.62f, 1.74f}},
-    {2, 1, 1, 0, 512, {5.97f, 0.944f, 15.9f, 14.0f, 1.11f, 2.95f, 3.18f}},
-    {2, 1, 1, 1, 256, {8.81f, 2.47f, 33.5f, 10.3f, 0.632f, 3.7f, 2.26f}},
-    {2, 1, 1, 2, 256, {11.4f, 0.964f, 59.2f, 18.6f, 0.3f, 4.44f, 1.87f}},
+    {2, 1, 1, 0, 512, {5.81f, 1.15f, 16.0f, 15.3f, 0.717f, 3.14f, 2.9f}},
+    {2, 1, 1, 1, 256, {8.79f, 2.53f, 33.5f, 11.5f, 0.58f, 3.8f, 2.19f}},
+    {2, 1, 1, 2, 256, {11.6f, 0.829f, 59.2f, 19.5f, 0.17f, 4.56f, 1.87f}},
+    {2, 1, 1, 4, 1280, {1.72f, 3.86f, 20.5f, 45.8f, 0.701f, 3.66f, 2.73f}},
+    {2, 1, 1, 5, 512, {9.81f, 0.0f, 38.3f, 40.2f, 0.277f, 4.27f, 1.78f}},
     {3, 0, 0, 0, 1536, {6.62f, 0.0f, 9.87f, 18.1f, 0.397f, 2.33f, 2.54f}},
     {3, 0, 0, 1, 768, {9.12f, 0.0f, 16.4f, 19.7f, 0.362f, 3.69f, 1.4f}},
-    {3, 0, 1, 0, 512, {5.56f, 1.34f, 3.94f, 5.76f, 0.476f, 2.8f, 2.89f}},
-    {3, 0, 1, 1, 256, {5.9f, 2.99f, 7.42f, 3.96f, 0.336f, 4.43f, 1.74f}},
-    {3, 0, 1, 2, 256, {7.05f, 1.96f, 10.5f, 7.67f, 0.35f, 5.19f, 1.39f}},
-    {3, 0, 1, 3, 256, {8.06f, 3.53f, 17.1f, 13.5f, 0.227f, 6.23f, 1.06f}},
+    {3, 0, 1, 0, 512, {5.54f, 1.42f, 3.67f, 6.03f, 0.456f, 2.82f, 3.01f}},
+    {3, 0, 1, 1, 256, {5.95f, 3.02f, 7.29f, 4.57f, 0.351f, 4.44f, 1.73f}},
+    {3, 0, 1, 2, 256, {7.17f, 1.86f, 10.3f, 8.14f, 0.376f, 4.97f, 1.41f}},
+    {3, 0, 1, 3, 256, {7.87f, 3.66f, 17.0f, 13.5f, 0.238f, 6.26f, 1.08f}},
+    {3, 0, 1, 4, 1024, {6.48f, 0.107f, 5.4f, 12.0f, 0.53f, 2.77f, 2.67f}},
+    {3, 0, 1, 5, 512, {7.98f, 0.517f, 8.49f, 11.6f, 0.434f, 4.84f, 1.38f}},
     {3, 1, 0, 0, 1536, {6.03f, 0.0f, 30.0f, 69.5f, 0.569f, 2.96f, 2.23f}},
     {3, 1, 0, 1, 512, {9.02f, 0.0f, 60.8f, 41.9f, 0.6f, 4.1f, 1.36f}},
-    {3, 1, 1, 0, 512, {5.38f, 1.29f, 16.9f, 16.1f, 0.946f, 3.34f, 2.54f}},
-    {3, 1, 1, 1, 256, {6.55f, 4.24f, 36.2f, 12.9f, 0.626f, 4.94f, 1.45f}},
-    {3, 1, 1, 2, 256, {8.34f, 3.51f, 63.1f, 21.4f, 0.593f, 6.24f, 1.18f}},
+    {3, 1, 1, 0, 512, {5.76f, 0.733f, 17.2f, 16.6f, 1.22f, 3.5f, 2.66f}},
+    {3, 1, 1, 1, 256, {6.45f, 4.21f, 36.6f, 13.2f, 0.673f, 4.81f, 1.57f}},
+    {3, 1, 1, 2, 256, {8.13f, 3.59f, 63.4f, 22.2f, 0.607f, 6.19f, 1.24f}},
+    {3, 1, 1, 4, 1280, {6.26f, 0.0f, 18.0f, 55.0f, 0.95f, 3.2f, 2.51f}},
+    {3, 1, 1, 5, 512, {10.1f, 0.0f, 37.8f, 44.6f, 0.846f, 5.05f, 1.42f}},
 };
 
 // one product of a model's kind
@@ -70,14 +86,14 @@ struct DenseShape {
     long long tiles, padded;
     int stages;
     DenseShape(const DenseModel& model, int M, int N, int stages_) : m(model), stages(stages_) {
-        static const int kRows[] = {64, 128, 256, 256}, kCols[] = {64, 128, 128, 256}, kPairCols[] = {64, 64, 64, 128};
+        static const int kRows[] = {64, 128, 256, 256, 64, 128}, kCols[] = {64, 128, 128, 256, 64, 128}, kPairCols[] = {64, 64, 64, 128, 64, 64};
         const bool pair = m.kind == kDensePair;
         const long long bm = kRows[m.tile], bn = (pair ? kPairCols : kCols)[m.tile];
         tiles = ((M + bm - 1) / bm) * ((N + bn - 1) / bn), padded = (tiles + kXcds - 1) / kXcds * kXcds;
         k = 1e-3 * stages * (m.f32 ? 32 : 64), sums = 1e-6 * M * N * (pair ? 2 : 1);
     }
     // two stages to a part, parts side by side
-    bool allowed(int parts) const { return parts == 1 || (parts * 2 <= stages && tiles * parts <= (m.direct ? 560 : 1200)); }
+    bool allowed(int parts) const { return parts == 1 || (parts * 2 <= stages && tiles * parts <= (m.direct && m.tile < kTileS2 ? 560 : 1200)); }
     double groups(int parts) const { return (double)(parts > 1 ? padded * parts : tiles); }
     double us(int parts) const {
         const double g = groups(parts);
@@ -109,7 +125,7 @@ DensePlan plan_dense(DenseKind kind, int M, int N, int stages, bool f32, bool di
     });
 }
 
-// Two products in one launch, fitted likewise to 69000 timings of 5500 pairs: fixed, a round; by 1000 elements of K a round of the mean workgroup, the work of all of them and the longest one; results; second, part.
+// Two products in one launch, fitted likewise to 68000 timings of 5400 pairs: fixed, a round; by 1000 elements of K a round of the mean workgroup, the work of all of them and the longest one; results; second, part.
 struct DenseTwoModel {
     int f32, direct, tile, slots;
     float us[8];
@@ -117,18 +133,22 @@ struct DenseTwoModel {
 static const DenseTwoModel kDenseTwoModels[] = {
     {0, 0, 0, 512, {5.3f, 0.413f, 0.528f, 4.79f, 10.6f, 0.0f, 3.59f, 2.04f}},
     {0, 0, 1, 1024, {7.29f, 1.09f, 1.8f, 22.2f, 15.5f, 0.0f, 4.11f, 1.47f}},
-    {0, 1, 0, 512, {6.35f, 1.39f, 0.0f, 7.46f, 2.65f, 0.0f, 2.67f, 2.57f}},
-    {0, 1, 1, 256, {7.64f, 2.42f, 1.33f, 6.54f, 4.41f, 0.0f, 3.31f, 1.83f}},
-    {0, 1, 2, 256, {7.99f, 1.77f, 2.51f, 8.62f, 7.4f, 0.0f, 3.85f, 1.49f}},
-    {0, 1, 3, 256, {8.68f, 3.1f, 2.18f, 13.2f, 14.5f, 0.0f, 4.75f, 1.24f}},
-    {1, 0, 0, 1536, {4.65f, 0.996f, 0.809f, 57.2f, 29.0f, 0.0f, 3.24f, 2.52f}},
+    {0, 1, 0, 512, {6.25f, 1.3f, 0.81f, 6.6f, 2.67f, 0.0373f, 2.68f, 2.79f}},
+    {0, 1, 1, 256, {7.64f, 2.16f, 2.02f, 5.71f, 4.46f, 0.03f, 3.58f, 1.84f}},
+    {0, 1, 2, 256, {8.07f, 1.54f, 3.16f, 8.15f, 7.46f, 0.0f, 4.11f, 1.48f}},
+    {0, 1, 3, 256, {8.59f, 3.05f, 2.66f, 12.7f, 14.4f, 0.0f, 5.01f, 1.2f}},
+    {0, 1, 4, 256, {6.16f, 0.372f, 1.0f, 1.82f, 5.31f, 0.0f, 3.25f, 1.92f}},
+    {0, 1, 5, 256, {7.69f, 0.862f, 0.194f, 6.22f, 7.86f, 0.0f, 4.22f, 1.29f}},
+    {1, 0, 0, 512, {5.35f, 0.302f, 0.933f, 18.3f, 29.0f, 0.0f, 3.26f, 2.43f}},
     {1, 0, 1, 512, {5.78f, 2.25f, 6.13f, 41.6f, 59.0f, 0.0f, 3.81f, 1.62f}},
-    {1, 1, 0, 512, {6.26f, 1.5f, 0.728f, 20.5f, 14.0f, 0.0f, 2.69f, 2.66f}},
-    {1, 1, 1, 256, {8.47f, 3.63f, 5.47f, 20.0f, 28.7f, 0.0f, 3.18f, 1.76f}},
-    {1, 1, 2, 256, {7.66f, 4.93f, 8.66f, 28.0f, 53.5f, 0.0f, 4.34f, 1.34f}},
+    {1, 1, 0, 256, {6.62f, 0.89f, 2.96f, 7.06f, 14.1f, 0.0f, 2.61f, 2.59f}},
+    {1, 1, 1, 256, {8.29f, 3.76f, 5.81f, 20.0f, 28.6f, 0.0f, 3.28f, 1.71f}},
+    {1, 1, 2, 256, {8.06f, 4.46f, 9.22f, 27.1f, 53.3f, 0.0f, 4.42f, 1.4f}},
+    {1, 1, 4, 256, {5.4f, 0.784f, 0.0f, 9.1f, 19.5f, 0.0f, 3.43f, 1.63f}},
+    {1, 1, 5, 256, {8.91f, 1.72f, 0.17f, 24.4f, 36.1f, 0.0611f, 4.05f, 1.19f}},
 };
 
-// One launch where it is expected to be ahead of two: on 9 of 10 of those pairs, by 20 % of both products on average (2 to 6 % behind the best tile and parts).
+// One launch where it is expected to be ahead of two: on 9 of 10 of those pairs, by 20 % of both products on average (1 to 3 % behind the best tile and parts).
 DensePlans plan_gradients(int B, int d_in, int K_stages, int rows, int B_stages, bool f32, bool direct) {
     struct Key { int32_t B, d_in, K_stages, rows, B_stages, form; };
     static thread_local DecisionCache<Key, DensePlans, 64> cache;
