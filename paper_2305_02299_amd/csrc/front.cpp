@@ -405,6 +405,15 @@ void of_type(const at::Tensor* t, bool ok, const char* what) {
     }
 }
 void* data(const at::Tensor* t) { return t ? t->data_ptr() : nullptr; }
+// A result given by the caller: not in an input's memory
+void apart(const at::Tensor* out, const at::Tensor* in, const char* what) {
+    if (!out || !in) return;
+    const auto *o = static_cast<const char*>(out->data_ptr()), *i = static_cast<const char*>(in->data_ptr());
+    if (o < i + in->nbytes() && i < o + out->nbytes()) {
+        PyErr_Format(PyExc_ValueError, "the result overlaps %s", what);
+        throw Failed{};
+    }
+}
 const float* floats(PyObject* o, const char* what, int64_t n) {
     const at::Tensor* t = shaped(o, what, {n}, true);
     of_type(t, t && t->scalar_type() == at::kFloat, what);
@@ -471,6 +480,9 @@ PyObject* structured_act(PyObject*, PyObject* const* a, Py_ssize_t n) {
         const srigl_dtype yt = given ? dtype_of(*given) : PyObject_IsTrue(a[7]) == 1 ? SRIGL_F32 : l.type;
         const at::Tensor* residual = shaped(a[5], "residual", {l.B, l.d_out}, true);
         of_type(residual, residual && dtype_of(*residual) == yt, "residual");
+        apart(given, l.x, "x");
+        apart(given, l.W, "the weight matrix");
+        if (residual && given && residual->data_ptr() != given->data_ptr()) apart(given, residual, "a part of the residual");
         at::Tensor made[2];
         if (!given) made[0] = fresh({l.B, l.d_out}, yt == SRIGL_F32 ? at::kFloat : l.x->scalar_type(), *l.x);
         if (save) made[1] = fresh({l.B, l.n}, l.x->scalar_type(), *l.x);

@@ -311,3 +311,22 @@ def test_refused_tensors():
         with pytest.raises((SriglError, TypeError, AssertionError, ValueError)):
             wrong()
     assert half_step(torch.bfloat16) == 2.0 ** -8
+
+
+def test_refused_results():
+    """A result in the memory of an input, or of another type than asked for; the residual itself is a place for it."""
+    gen = torch.Generator().manual_seed(5)
+    memory = normal(gen, (3, 20, 64), 1.0, torch.float32).cuda()
+    x, W, residual = memory[0], normal(gen, (64, 64), 0.1, torch.float32).cuda(), memory[1]
+    layer = StructuredLinear(64, 64, W)
+    want = layer.forward(x, residual=residual)
+    for kw in (dict(y=x), dict(y=W[:20]), dict(y=memory.view(-1)[20 * 64 - 64:2 * 20 * 64 - 64].view(20, 64)),
+               dict(y=memory.view(-1)[2 * 20 * 64 - 64:3 * 20 * 64 - 64].view(20, 64), residual=residual)):
+        with pytest.raises(ValueError):
+            layer.forward(x, **kw)
+    half = StructuredLinear(64, 64, W.bfloat16())
+    with pytest.raises(AssertionError):
+        half.forward(x.bfloat16(), out_dtype=torch.float32, y=torch.empty(20, 64, dtype=torch.bfloat16, device="cuda"))
+    y = memory[2]
+    assert layer.forward(x, residual=residual, y=y) is not None and torch.equal(y, want)
+    assert torch.equal(layer.forward(x, residual=residual, y=residual), want) and torch.equal(residual, want)
