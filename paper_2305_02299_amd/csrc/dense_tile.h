@@ -747,7 +747,7 @@ __device__ __forceinline__ void load_values(const T* p, float (&v)[V], int valid
 // The activations of these products and their slopes, for millions of values behind a product: one hardware exponential (of two) and one reciprocal each.
 // GELU: Phi(-|v|) = erfc(|v| / sqrt 2) / 2 by Abramowitz and Stegun 7.1.26, a polynomial of degree 5 in t = 1 / (1 + p |v| / sqrt 2) times exp(-v^2 / 2), which is the density's exponential
 // too; |error of erf| <= 1.5e-7, a step or two of fp32 beside 1.  (With erff the epilogue of 2048 x 13108 values was 40 us of vector instructions.)
-// SiLU: the exponential is off by |v| 2^-24 of itself, the reciprocal by a step.  NaN stays NaN in all of them.
+// SiLU: the exponential is off by |v| 2^-24 of itself, the reciprocal by a step.  NaN stays NaN in all of them (ReLU's slope there is 0).
 __device__ __forceinline__ float exp_of(float v) { return __builtin_amdgcn_exp2f(v * 1.44269504088896340736f); }
 __device__ __forceinline__ float logistic(float v) { return __builtin_amdgcn_rcpf(1.0f + exp_of(-v)); }
 // Phi(-|v|), and exp(-v^2 / 2)
