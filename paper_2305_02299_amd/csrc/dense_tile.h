@@ -634,8 +634,8 @@ __device__ __forceinline__ TileColumns listed_columns(int n0, const Out& out) {
 template <int BM, int BN, int WGM, int WGN, int V, class Out>
 __device__ __forceinline__ void listed_as_rows(unsigned char* smem, unsigned char* tables, const f32x16_t (&acc)[BM / WGM / 32][BN / WGN / 32], int m0, int n0, int M, Out& out) {
     using EL = EpiLayout<BN, WGM>;
-    constexpr int NT = WGM * WGN * 64, TM = BM / WGM / 32, TN = BN / WGN / 32, PITCH = EL::PITCH, GROUPS = EL::COLS / V, STEP = NT / GROUPS;
-    static_assert(NT % GROUPS == 0 && EL::COLS >= BN, "a thread keeps its columns");
+    constexpr int NT = WGM * WGN * 64, TM = BM / WGM / 32, TN = BN / WGN / 32, PITCH = EL::PITCH;
+    static_assert(NT >= EL::COLS / V && EL::COLS >= BN, "columns to the threads");
     float* const tile = reinterpret_cast<float*>(smem);
     const int* const place = reinterpret_cast<const int*>(tables);
     const int* const table = place + BN;
@@ -676,7 +676,9 @@ __device__ __forceinline__ void listed_as_rows(unsigned char* smem, unsigned cha
             if (at[j] >= wc) at[j] = -1;
             add[j] = tbias[max(at[j], 0)];
         }
-        const int k0 = (tid % GROUPS) * V, first = max(head - k0, 0), valid = min(V, wc - k0);
+        // As many threads to a row as the window has columns for, those behind the last whole row of threads idle: a thread keeps its V columns, and none works on columns behind the range, which is 1.25 tile widths
+        // with a fifth ablated and the window two (bf16 4096 -> 16384 at 2048 rows with GELU, a fifth ablated, 272 -> 253 us; 104 -> 3001, half ablated, 500 rows in 128 x 128 tiles 37 -> 25).
+        const int groups = (wc + V - 1) / V, step = NT / groups, k0 = (tid % groups) * V, first = max(head - k0, 0), valid = tid < step * groups ? min(V, wc - k0) : 0;
         int gaps = 0;
         float flat[V];
 #pragma unroll
@@ -697,7 +699,7 @@ __device__ __forceinline__ void listed_as_rows(unsigned char* smem, unsigned cha
                     for (int e = 0; e < 16; ++e) t[(8 * (e >> 2) + (e & 3)) * PITCH] = acc[i][j][e] + add[j];
                 }
             __syncthreads();
-            for (int r = tid / GROUPS; r < 32 * WGM; r += STEP) {
+            for (int r = tid / groups; r < 32 * WGM; r += step) {
                 const int m = m0 + (r >> 5) * (BM / WGM) + i * 32 + (r & 31);
                 if (m >= M || valid <= first) continue;
                 float v[V];
