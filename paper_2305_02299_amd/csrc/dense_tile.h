@@ -752,11 +752,11 @@ __device__ __forceinline__ void load_values(const T* p, float (&v)[V], int valid
 // SiLU: the exponential is off by |v| 2^-24 of itself, the reciprocal by a step.  NaN stays NaN in all of them (ReLU's slope there is 0).
 __device__ __forceinline__ float exp_of(float v) { return __builtin_amdgcn_exp2f(v * 1.44269504088896340736f); }
 __device__ __forceinline__ float logistic(float v) { return __builtin_amdgcn_rcpf(1.0f + exp_of(-v)); }
-// Phi(-|v|), and exp(-v^2 / 2)
+// Phi(-|v|), and exp(-v^2 / 2)  (1 / sqrt 2, 1 / 2 and the exponential's log2 e are in the constants)
 __device__ __forceinline__ float normal_tail(float v, float* e) {
-    const float x = fabsf(v) * 0.70710678118654752440f, t = __builtin_amdgcn_rcpf(fmaf(0.3275911f, x, 1.0f));
-    *e = exp_of(-0.5f * v * v);
-    return 0.5f * *e * t * fmaf(t, fmaf(t, fmaf(t, fmaf(t, 1.061405429f, -1.453152027f), 1.421413741f), -0.284496736f), 0.254829592f);
+    const float t = __builtin_amdgcn_rcpf(fmaf(0.23164189f, fabsf(v), 1.0f));
+    *e = __builtin_amdgcn_exp2f(-0.72134752044448170368f * v * v);
+    return *e * t * fmaf(t, fmaf(t, fmaf(t, fmaf(t, 0.5307027145f, -0.7265760135f), 0.7107068705f), -0.142248368f), 0.127414796f);
 }
 __device__ __forceinline__ float act_value(float v, int act) {
     if (act == SRIGL_ACT_SILU) return v * logistic(v);
