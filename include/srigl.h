@@ -478,8 +478,8 @@ srigl_status srigl_structured_linear_fwd_split(const void* x, srigl_dtype x_dtyp
  * overwritten, in rounding to nearest, and not aliasing inputs unless said otherwise; workspace: device memory of the caller, 16-byte aligned, at least as many bytes as the
  * call's query says (host arithmetic on the same sizes; NULL where that is 0), contents undefined afterwards, SRIGL_ERR_CAPACITY where it is
  * smaller.  Calls that share one must not overlap.  No call synchronises, allocates or uses atomics: the same inputs give the same bits.
- * fp32 products of more rows of x than a few run as three bf16 parts of every value, six products a pair, as exact as fp32 sums are (what is left out is below 2^-23 of a product), but a value
- * below 2^-110 loses its last bits; a tile with a sum that is not finite is computed again in fp32.  Infinities and NaN follow the formulas as they stand (an infinite dy times a slope of 0 is NaN).
+ * fp32 products of more rows of x than a few run as three bf16 parts of every value, six products a pair: what is left out is at most 2^-24 of a product, of either sign; a value below 2^-110 loses its last
+ * bits; a tile with a sum that is not finite is computed again in fp32.  Infinities and NaN follow the formulas as they stand (an infinite dy times a slope of 0 is NaN).
  *
  * srigl_structured_linear_fwd_act:
  *   z[b][s] = bias[active[s]] + sum_j Wd[s][j] x[b][j];  y[b][active[s]] = act(z[b][s]) + residual[b][active[s]];  other columns: act(bias[c]) + residual[b][c].

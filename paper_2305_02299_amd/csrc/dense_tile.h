@@ -18,7 +18,9 @@
 
 namespace srigl {
 
+typedef float f32x2_t __attribute__((ext_vector_type(2)));
 typedef float f32x4_t __attribute__((ext_vector_type(4)));
+typedef __bf16 bf16x2_t __attribute__((ext_vector_type(2)));
 typedef short s16x4_t __attribute__((ext_vector_type(4)));
 
 template <typename T> struct DenseFrag;
@@ -216,11 +218,14 @@ struct FragReader {
 };
 
 // ---- fp32 on the bf16 units ----
-// An fp32 value is exactly the sum of three bf16 values, its upper, middle and lower eight bits (cut off, not rounded).  Of the nine products of two values the six that reach 2^-16 of the first go through
-// the bf16 units into the same fp32 sums; what is left out is below 2^-23 of the product (2^-25 on average), and sixteen products meet in one rounding where the fp32 instructions round every two.  Six
-// instructions of 32 clocks do what the fp32 ones do in 512 (2.7 times as fast); the lanes cut the values on their way from the LDS, 5.5 instructions a value, between the multiplications.  (Middle and lower
-// bits below 2^-126 count as zero: a value below 2^-110 loses its last bits, as far as its products matter beside others'.)  Infinities and NaN come out as NaN, and so does a sum that
-// leaves the range on its way: a tile with a sum that is not finite is computed again by the fp32 instructions.
+// An fp32 value is exactly the sum of three bf16 values, each what the ones before leave, the first two rounded to nearest: the second is at most 2^-8 of the value's power of two, the third 2^-17, in seven
+// bits.  Of the nine products of two values the six that reach 2^-17 of the first go through the bf16 units into the same fp32 sums; what is left out is at most 2^-24 of the product, half a step of fp32,
+// and of either sign.  (Cut off in place of rounded, the parts are up to 2^-7 and 2^-15, all of the value's sign: up to 2^-21 of a product was left out, always towards zero.  Rounding costs what a
+// conversion takes more than a byte permutation, in a longer chain: 768 -> 3072 at 512 rows 27.6 us, now 29.8, its gradients 51.0 and 52.9, 4096 -> 4096 at 2048 rows 336 and 337; the second part cut off, 2^-23,
+// 29.1, 52.4 and 335.)  A product by itself came out within 2.2 half steps, the units' own rounding among them.  Six instructions of 32 clocks do what the fp32 ones do in 512 (2.7 times as fast), and sixteen
+// products meet in one rounding where the fp32 instructions round every two; the lanes split the values on their way from the LDS, 5.5 instructions a value, between the multiplications.  (The units take bf16
+// denormals as they are, down to 2^-133: a value below 2^-110 loses its last bits, as far as its products matter beside others'.)  Infinities, NaN and values that round beyond bf16's range come out as NaN, and so
+// does a sum that leaves the range on its way: a tile with a sum that is not finite is computed again by the fp32 instructions.
 template <bool ALONG, int R, int TB>
 struct SplitReader {
     static constexpr int PITCH = R * 4;
@@ -252,13 +257,13 @@ struct SplitFrag { uint32_t part[3][4]; };
 __device__ __forceinline__ void split_pair(SplitFrag& f, const f32x4_t (&v)[2], int i) {
     float x = v[i >> 1][2 * (i & 1)], y = v[i >> 1][2 * (i & 1) + 1];
 #pragma unroll
-    for (int p = 0; p < 3; ++p) {
-        f.part[p][i] = __builtin_amdgcn_perm(__float_as_uint(y), __float_as_uint(x), 0x07060302u);   // the upper halves of both
-        if (p < 2) {
-            x -= __uint_as_float(__float_as_uint(x) & 0xffff0000u);
-            y -= __uint_as_float(__float_as_uint(y) & 0xffff0000u);
-        }
+    for (int p = 0; p < 2; ++p) {
+        const uint32_t both = __builtin_bit_cast(uint32_t, __builtin_convertvector(f32x2_t{x, y}, bf16x2_t));   // to nearest
+        f.part[p][i] = both;
+        x -= __uint_as_float(both << 16);
+        y -= __uint_as_float(both & 0xffff0000u);
     }
+    f.part[2][i] = __builtin_amdgcn_perm(__float_as_uint(y), __float_as_uint(x), 0x07060302u);   // the upper halves of both: there is nothing in the lower ones
 }
 __device__ __forceinline__ bf16x8_t split_part(const SplitFrag& f, int p) { return __builtin_bit_cast(bf16x8_t, *reinterpret_cast<const uint4*>(f.part[p])); }
 
