@@ -311,7 +311,7 @@ static srigl_status linear_bwd(const BwdPlan& p, const void* dy, const void* x, 
     // without an activation or ablated neurons dz is dy: only its column sums are left to do
     const bool as_it_is = std::is_same<T, TY>::value && act == SRIGL_ACT_NONE && n == d_out && n % kPiece<T> == 0 && !astray(16, {dy});
     const bool listed = n < d_out;
-    if (p.chunks > 0 && (n > 0 || dbias) && (!as_it_is || dbias)) {
+    if (p.chunks > 0 && d_out > 0 && (n > 0 || dbias) && (!as_it_is || dbias)) {
         constexpr int COLS = kDzCols * kPiece<T>;
         T* const to = as_it_is || n == 0 ? nullptr : dz;
         float* const sum_to = dbias ? sums : nullptr;

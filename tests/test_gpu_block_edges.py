@@ -1,0 +1,18 @@
+"""Calls of the feed-forward blocks at the ends of what their sizes and arguments allow."""
+import pytest
+import torch
+
+from paper_2305_02299_amd import binding as B_
+
+pytestmark = pytest.mark.gpu
+
+
+@pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16])
+def test_a_layer_without_outputs(dtype):
+    """d_out of 0: there is no gradient to take in, dx is zero, and the bias's gradient has no element, wherever it is said to stand."""
+    B, d_in = 5, 24
+    x, W, dy = (torch.ones(s, device="cuda", dtype=dtype) for s in ((B, d_in), (1, d_in), (B, 1)))
+    dx, dW, db = torch.full((B, d_in), 7.0, device="cuda", dtype=dtype), torch.full((1, d_in), 7.0, device="cuda", dtype=dtype), torch.full((4,), 7.0, device="cuda")
+    ws = torch.empty(max(B_.srigl_structured_bwd_workspace_bytes(B, d_in, 0, 0, B_._dtype_code(x)), 16), dtype=torch.uint8, device="cuda")
+    B_.srigl_structured_linear_bwd(dy, x, B, d_in, W, None, 0, db, None, 0, dx, dW, db, ws)
+    assert not dx.any() and (dW == 7).all() and (db == 7).all()
