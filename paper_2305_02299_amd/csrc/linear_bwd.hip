@@ -273,14 +273,18 @@ struct BwdPlan {
     size_t dz_bytes, sum_bytes, dx_part_bytes, bytes;   // in this order, the parts of dW's product last
 };
 static size_t whole(size_t bytes) { return (bytes + 255) / 256 * 256; }
-// cols: columns of dz in a row, padding included; K: what dx's product sums over; dW_rows: rows of the weight gradients' product; sum_cols: columns of the sums
-static BwdPlan plan_bwd(int B, int d_in, long long cols, long long K, long long dW_rows, long long sum_cols, size_t elem) {
+enum class DzPass { kPlain, kListed, kPair };
+// cols: columns of dz in a row, padding included (kPair: of dg and du, a thread takes the same ones of both); K: what dx's product sums over; dW_rows: rows of the weight gradients' product; sum_cols: columns of
+// the sums
+static BwdPlan plan_bwd(DzPass pass, int B, int d_in, long long cols, long long K, long long dW_rows, long long sum_cols, size_t elem) {
     BwdPlan p{};
     const bool f32 = elem == 4, direct = d_in % (16 / (int)elem) == 0;
 
-    // about 2048 workgroups, two to eight rows to a thread and more only where the grid would be too large
-    const long long per_group = kDzCols * 16 / (long long)elem, groups = std::max(1ll, (cols / (dW_rows == cols ? 2 : 1) + per_group - 1) / per_group);
-    long long rows = std::min<long long>(8, std::max<long long>(2, B * groups / (2048 * kDzRows))) * kDzRows;
+    // About 4096 workgroups of k_dz_linear, whatever the width (gradients of a layer 256 -> 4096, fp32 at 2048 rows, 81.8 us against 87.3 with 2048, bf16 at 8192 rows 90.8 and 91.8, 256 -> 16384 at 2048 rows 87.7 and
+    // 86.8, 256 -> 3001 at 4096 45.3 and 44.4), 2048 of the others (a fifth of 16384 neurons ablated, 4096 -> 16384 at 2048 rows, 476 us against 495 with 4096); two to eight rows to a thread and more only where the
+    // grid would be too large
+    const long long per_group = kDzCols * 16 / (long long)elem, groups = std::max(1ll, (cols / (pass == DzPass::kPair ? 2 : 1) + per_group - 1) / per_group);
+    long long rows = std::min<long long>(8, std::max<long long>(2, B * groups / ((pass == DzPass::kPlain ? 4096 : 2048) * kDzRows))) * kDzRows;
     rows = std::max<long long>(rows, ((long long)B + 65534) / 65535);
     p.chunk_rows = (int)std::min<long long>(rows, kMaxSide);
     p.chunks = (int)((B + (long long)p.chunk_rows - 1) / p.chunk_rows);
@@ -358,7 +362,7 @@ extern "C" {
 
 size_t srigl_structured_bwd_workspace_bytes(int32_t B, int32_t d_in, int32_t n_active, int32_t d_out, srigl_dtype dtype) {
     if (B < 0 || d_in < 0 || n_active < 0 || d_out < n_active || !known_dtype(dtype) || !bwd_sizes_fit(B, d_in, d_out)) return 0;
-    return plan_bwd(B, d_in, padded(n_active), n_active, n_active, d_out, dtype_bytes(dtype)).bytes;
+    return plan_bwd(n_active < d_out ? DzPass::kListed : DzPass::kPlain, B, d_in, padded(n_active), n_active, n_active, d_out, dtype_bytes(dtype)).bytes;
 }
 
 srigl_status srigl_structured_linear_bwd(const void* dy, srigl_dtype dy_dtype, const void* x, srigl_dtype x_dtype, int32_t B, int32_t d_in, const void* Wd,
@@ -374,7 +378,7 @@ srigl_status srigl_structured_linear_bwd(const void* dy, srigl_dtype dy_dtype, c
     if (rows && act != SRIGL_ACT_NONE && z == nullptr && (dx || dWd || dbias)) return SRIGL_ERR_INVALID_ARG;
     if (astray(dtype_bytes(x_dtype), {x, Wd, z, dx, dWd}) || astray(dtype_bytes(dy_dtype), {dy}) || astray(4, {bias, active, dbias})) return SRIGL_ERR_INVALID_ARG;
     if (!dx && !dWd && !dbias) return SRIGL_OK;
-    const BwdPlan p = plan_bwd(B, d_in, padded(n_active), n_active, n_active, d_out, dtype_bytes(x_dtype));
+    const BwdPlan p = plan_bwd(n_active < d_out ? DzPass::kListed : DzPass::kPlain, B, d_in, padded(n_active), n_active, n_active, d_out, dtype_bytes(x_dtype));
     if (p.bytes > 0 && workspace == nullptr) return SRIGL_ERR_CAPACITY;
     if (workspace_bytes < p.bytes) return SRIGL_ERR_CAPACITY;
     if ((reinterpret_cast<uintptr_t>(workspace) & 15) != 0) return SRIGL_ERR_INVALID_ARG;
@@ -388,7 +392,7 @@ srigl_status srigl_structured_linear_bwd(const void* dy, srigl_dtype dy_dtype, c
 
 size_t srigl_gated_bwd_workspace_bytes(int32_t B, int32_t d_in, int32_t n, srigl_dtype dtype) {
     if (B < 0 || d_in < 0 || n < 0 || !known_dtype(dtype) || !bwd_sizes_fit(B, d_in, n)) return 0;
-    return plan_bwd(B, d_in, 2 * padded(n), 2 * padded(n), 2 * padded(n), 2ll * n, dtype_bytes(dtype)).bytes;
+    return plan_bwd(DzPass::kPair, B, d_in, 2 * padded(n), 2 * padded(n), 2 * padded(n), 2ll * n, dtype_bytes(dtype)).bytes;
 }
 
 srigl_status srigl_gated_linear_bwd(const void* dh, const void* x, srigl_dtype x_dtype, int32_t B, int32_t d_in, const void* Wg, const void* Wu, srigl_dtype w_dtype,
@@ -401,7 +405,7 @@ srigl_status srigl_gated_linear_bwd(const void* dh, const void* x, srigl_dtype x
     if (rows && d_in > 0 && ((dx && (Wg == nullptr || Wu == nullptr)) || ((dWg || dWu) && x == nullptr))) return SRIGL_ERR_INVALID_ARG;
     if (astray(dtype_bytes(x_dtype), {dh, x, Wg, Wu, g, u, dx, dWg, dWu}) || astray(4, {dbias_g, dbias_u})) return SRIGL_ERR_INVALID_ARG;
     if (!any) return SRIGL_OK;
-    const BwdPlan p = plan_bwd(B, d_in, 2 * padded(n), 2 * padded(n), 2 * padded(n), 2ll * n, dtype_bytes(x_dtype));
+    const BwdPlan p = plan_bwd(DzPass::kPair, B, d_in, 2 * padded(n), 2 * padded(n), 2 * padded(n), 2ll * n, dtype_bytes(x_dtype));
     if (workspace_bytes < p.bytes || (p.bytes > 0 && workspace == nullptr)) return SRIGL_ERR_CAPACITY;
     if ((reinterpret_cast<uintptr_t>(workspace) & 15) != 0) return SRIGL_ERR_INVALID_ARG;
     hipStream_t st = static_cast<hipStream_t>(stream);
