@@ -51,15 +51,21 @@ class CondensedLinear:
             B_.srigl_block_terms(self.W_c, self.idx, self.seg, self.n_active, self.K, self.d_in, self.blocked)
         return self
 
+    def _densify(self, rows: int) -> torch.Tensor:
+        Wd = torch.empty((rows, self.d_in), dtype=self.W_c.dtype, device=self.W_c.device)
+        if rows:
+            B_.srigl_densify(self.W_c, self.idx if self.idx_wide is None else self.idx_wide, self.n_active, self.K, self.d_in, Wd)
+        return Wd
+
     def dense_rows(self) -> torch.Tensor:
         if self.Wd is None:
-            self.Wd = torch.empty((max(self.n_active, 1), self.d_in), dtype=self.W_c.dtype, device=self.W_c.device)
-            B_.srigl_densify(self.W_c, self.idx if self.idx_wide is None else self.idx_wide, self.n_active, self.K, self.d_in, self.Wd)
+            self.Wd = self._densify(max(self.n_active, 1))
         return self.Wd
 
     def structured(self) -> "StructuredLinear":
-        """The layer as dense rows of its stored neurons (dense_rows(), a copy), with activation, residual and gradients."""
-        return StructuredLinear(self.d_in, self.d_out, self.dense_rows()[:self.n_active], self.active, self.bias)
+        """The layer as dense rows of its stored neurons, as W_c stands now, in memory of their own (training them leaves this layer's as they are; active and bias
+        are shared), with activation, residual and gradients."""
+        return StructuredLinear(self.d_in, self.d_out, self._densify(self.n_active), self.active, self.bias)
 
     def choose(self, batch: int) -> int:
         return B_.srigl_choose_representation(batch, self.d_in, self.n_active, self.K, self.d_out, B_._dtype_code(self.W_c))[0]

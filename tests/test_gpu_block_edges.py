@@ -16,3 +16,21 @@ def test_a_layer_without_outputs(dtype):
     ws = torch.empty(max(B_.srigl_structured_bwd_workspace_bytes(B, d_in, 0, 0, B_._dtype_code(x)), 16), dtype=torch.uint8, device="cuda")
     B_.srigl_structured_linear_bwd(dy, x, B, d_in, W, None, 0, db, None, 0, dx, dW, db, ws)
     assert not dx.any() and (dW == 7).all() and (db == 7).all()
+
+
+@pytest.mark.parametrize("ablate", [0.0, 0.4, 1.0])
+def test_dense_rows_of_their_own(ablate):
+    """structured() takes the weights as they stand, and what becomes of its rows is nothing to the condensed layer."""
+    import synth_inputs as si
+    from gpu_util import dev
+    from paper_2305_02299_amd import condense_layer
+    L = si.make_layer(96, 40, 12, 80, ablate_frac=min(ablate, 0.4), seed=3)
+    mask = L.mask * 0 if ablate == 1.0 else L.mask
+    layer, x = condense_layer(dev(L.W), dev(mask), L.K, dev(L.bias)), dev(L.x)
+    before = layer.dense_rows().clone()
+    layer.W_c.mul_(2)
+    rows = layer.structured()
+    assert rows.Wd.shape == (layer.n_active, 96) and torch.equal(rows.Wd, 2 * before[:layer.n_active])
+    rows.Wd.zero_()
+    assert torch.equal(layer.dense_rows(), before) and torch.equal(layer.structured().Wd, 2 * before[:layer.n_active])
+    assert layer.structured().forward(x).shape == (80, 40)
