@@ -482,6 +482,8 @@ PyObject* structured_act(PyObject*, PyObject* const* a, Py_ssize_t n) {
         of_type(residual, residual && dtype_of(*residual) == yt, "residual");
         apart(given, l.x, "x");
         apart(given, l.W, "the weight matrix");
+        apart(given, l.active, "active");
+        apart(given, tensor(a[3]), "the bias");
         if (residual && given && residual->data_ptr() != given->data_ptr()) apart(given, residual, "a part of the residual");
         at::Tensor made[2];
         if (!given) made[0] = fresh({l.B, l.d_out}, yt == SRIGL_F32 ? at::kFloat : l.x->scalar_type(), *l.x);

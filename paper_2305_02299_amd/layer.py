@@ -181,7 +181,7 @@ class StructuredLinear:
 
     def forward(self, x: torch.Tensor, act: int = B_.ACT_NONE, residual: torch.Tensor | None = None, out_dtype: torch.dtype | None = None,
                 save: bool = False, y: torch.Tensor | None = None):
-        """act(x Wd^T + bias) + residual, [batch, d_out]; out_dtype: x's (default) or fp32, and the residual's; y: where to put it, of that type (may be the residual; not x's memory).
+        """act(x Wd^T + bias) + residual, [batch, d_out]; out_dtype: x's (default) or fp32, and the residual's; y: where to put it, of that type (may be the residual; not in the memory of anything else that the call reads).
         save: returns (y, z), z the pre-activations [batch, n_active] that backward takes."""
         assert x.dim() == 2 and x.shape[1] == self.d_in, "x is [batch, d_in]"
         assert out_dtype in (None, x.dtype, torch.float32), "the result is of x's type or fp32"

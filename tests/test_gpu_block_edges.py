@@ -2,6 +2,7 @@
 import pytest
 import torch
 
+from paper_2305_02299_amd import StructuredLinear
 from paper_2305_02299_amd import binding as B_
 
 pytestmark = pytest.mark.gpu
@@ -34,3 +35,25 @@ def test_dense_rows_of_their_own(ablate):
     rows.Wd.zero_()
     assert torch.equal(layer.dense_rows(), before) and torch.equal(layer.structured().Wd, 2 * before[:layer.n_active])
     assert layer.structured().forward(x).shape == (80, 40)
+
+
+def test_a_result_in_the_memory_of_the_bias_or_the_list():
+    """Refused before anything is launched: what is there stays."""
+    room = torch.arange(200, device="cuda", dtype=torch.float32)
+    bias, x, W = room[50:80], torch.ones(2, 8, device="cuda"), torch.ones(30, 8, device="cuda")
+    for first in (0, 30, 79):
+        with pytest.raises(ValueError):
+            StructuredLinear(8, 30, W, None, bias).forward(x, y=room[first:first + 60].view(2, 30))
+    assert torch.equal(room, torch.arange(200, device="cuda", dtype=torch.float32))
+    y = room[80:140].view(2, 30)   # right behind it
+    assert (StructuredLinear(8, 30, W, None, bias).forward(x, y=y) == 8 + bias).all()
+    active = torch.arange(64, device="cuda", dtype=torch.int32)[:20]
+    layer = StructuredLinear(8, 30, W[:20], active)
+    with pytest.raises(ValueError):
+        layer.forward(x[:1], y=_over(active, 30))
+    assert active.tolist() == list(range(20))
+
+
+def _over(t, n):
+    """A float [1, n] that begins where t does"""
+    return torch.empty(0, dtype=torch.float32, device="cuda").set_(t.view(torch.float32).untyped_storage(), 0, (1, n))
