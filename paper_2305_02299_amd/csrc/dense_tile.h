@@ -812,6 +812,15 @@ __device__ __forceinline__ void act_slopes(const float (&v)[V], float (&slope)[V
 }
 
 // ---- kernel and launch ----
+// A dimension of a grid ends below 2^32 threads: more workgroups of so many threads than that stand in `times` layers of x each (whole eights, so that a workgroup's die is the one that tile_of_workgroup
+// expects; those behind the last one find nothing to do).
+struct GridLayers { unsigned x, times; };
+inline GridLayers grid_layers(long long groups, int threads) {
+    const long long most = ((1ll << 32) - 1) / threads / kXcds * kXcds, times = std::max(1ll, (groups + most - 1) / most), x = (groups + times - 1) / times;
+    return {(unsigned)(times == 1 ? x : (x + kXcds - 1) / kXcds * kXcds), (unsigned)times};
+}
+constexpr long long kMostGroups = 0x7fffff00ll;   // numbers of workgroups are ints
+
 // Sums of a part of K, [parts][M][N] (of a pair: [parts][M][2 N], the second's behind the first's)
 struct PartOut {
     static constexpr bool kListed = false;
@@ -928,7 +937,9 @@ __device__ __forceinline__ void dense_tile(unsigned char* smem, int id, int part
 template <typename T, int BM, int BN, int WGM, int WGN, int NS, bool PAIR, class P>
 __global__ __launch_bounds__(WGM * WGN * 64) void k_dense(P p) {
     extern __shared__ __attribute__((aligned(1024))) unsigned char smem[];
-    dense_tile<T, BM, BN, WGM, WGN, NS, PAIR>(smem, blockIdx.x, blockIdx.y, p);
+    int id = blockIdx.x;
+    if (blockIdx.z) id += (int)(blockIdx.z * gridDim.x);
+    dense_tile<T, BM, BN, WGM, WGN, NS, PAIR>(smem, id, blockIdx.y, p);
 }
 
 // Two products that do not wait for each other in one launch (the gradients of x and of W): what one leaves idle the other takes, and a small pass is a launch shorter.  The first one's workgroups come
@@ -1003,8 +1014,9 @@ static srigl_status launch_tiles(const DenseProduct<OA, OB, Out>& p, hipStream_t
     static LdsLimit limit;
     if (limit.ensure(kern, lds) != SRIGL_OK) return SRIGL_ERR_HIP;
     const long long n_wg = dense_groups<BM, PAIR ? BN / 2 : BN>(p);
-    if (n_wg > 0x7fffffffll || p.parts < 1 || p.parts > 65535) return SRIGL_ERR_UNSUPPORTED;
-    hipLaunchKernelGGL(kern, dim3((unsigned)n_wg, (unsigned)p.parts), dim3(WGM * WGN * 64), lds, st, p);
+    if (n_wg > kMostGroups || p.parts < 1 || p.parts > 65535) return SRIGL_ERR_UNSUPPORTED;
+    const GridLayers grid = grid_layers(n_wg, WGM * WGN * 64);
+    hipLaunchKernelGGL(kern, dim3(grid.x, (unsigned)p.parts, grid.times), dim3(WGM * WGN * 64), lds, st, p);
     if (p.parts > 1) {
         bool one = false;   // a neuron to a thread, which writes the ablated columns in front of its own too
         if constexpr (Out::kListed) {
@@ -1022,7 +1034,7 @@ static srigl_status launch_tiles_two(const P& p, const Q& q, const More& more, h
     static LdsLimit limit;
     if (limit.ensure(kern, lds) != SRIGL_OK) return SRIGL_ERR_HIP;
     const long long p_wg = dense_groups<BM, BN>(p), q_wg = dense_groups<BM, BN>(q), all = p_wg * p.parts + q_wg * q.parts + more.groups();
-    if (all > 0x7fffffffll) return SRIGL_ERR_UNSUPPORTED;
+    if (all * WGM * WGN * 64 >= 1ll << 32) return SRIGL_ERR_UNSUPPORTED;   // (pairs of products beyond a quarter of a millisecond don't come here)
     hipLaunchKernelGGL(kern, dim3((unsigned)all), dim3(WGM * WGN * 64), lds, st, p, q, (int)p_wg, (int)q_wg, more);
     const long long pj = join_groups(p, 4), qj = join_groups(q, 4);
     if (pj + qj > 0) hipLaunchKernelGGL((k_dense_join_two<P, Q>), dim3((unsigned)(pj + qj)), dim3(256), 0, st, p, q, (unsigned)pj);
@@ -1096,7 +1108,12 @@ template <typename T, int NB, int NW, bool PAIR, int UNITS, class Out>
 __global__ __launch_bounds__(NW * 64) void k_dense_few(const T* __restrict__ x, int B, int K, const T* __restrict__ W, long long to_second, int n, int rows, Out out) {
     constexpr int MATS = PAIR ? 2 : 1, STEP = 64 / (int)sizeof(T), UNIT = 2 * STEP, P = kPiece<T>;
     __shared__ float sums[NW][MATS][16][17];   // [neuron][row of x], of 16 rows of x at a time
-    const int lane = threadIdx.x & 63, wv = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), s0 = blockIdx.x * rows;
+    const int lane = threadIdx.x & 63, wv = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    int s0 = (int)blockIdx.x * rows;
+    if (blockIdx.y) {
+        s0 += (int)(blockIdx.y * gridDim.x) * rows;
+        if (s0 >= n) return;
+    }
     const T *w[MATS], *xr[NB];
     const int off = (lane >> 4) * P;
     w[0] = W + (size_t)min(s0 + min(lane & 15, rows - 1), n - 1) * K + off;
@@ -1166,8 +1183,9 @@ static srigl_status launch_few(const T* x, int B, int K, const T* W, long long t
     // Few neurons: four of them to a workgroup (the others' places in the matrix units repeat the last one), since a compute unit alone brings in little: bf16 3072 -> 768 at one row 4.6 us against 5.8 with
     // 16, 1024 -> 1024 2.7 and 3.0, but 768 -> 3072 3.9 and 3.2.
     const int rows = n >= 2048 ? 16 : 4;
-    const dim3 grid((unsigned)((n + (long long)rows - 1) / rows));
     const bool wide = (long long)K * (int)sizeof(T) >= 20 * 128;   // eight wavefronts to a line, else four (bf16 4096 -> 16384 at one row 24.8 us, 27.3 with four)
+    const GridLayers layers = grid_layers((n + (long long)rows - 1) / rows, wide ? 512 : 256);
+    const dim3 grid(layers.x, layers.times);
 #define SRIGL_FEW(NB, UNITS) \
     do { \
         if (wide) hipLaunchKernelGGL((k_dense_few<T, NB, 8, PAIR, UNITS, Out>), grid, dim3(512), 0, st, x, B, K, W, to_second, n, rows, out); \

@@ -240,7 +240,9 @@ struct SumChunks {
 };
 __global__ __launch_bounds__(256) void k_sum_chunks(SumChunks s) {
     __shared__ unsigned char held[4 * 64 * sizeof(float)];
-    s(held, blockIdx.x);
+    int group = blockIdx.x;
+    if (blockIdx.y) group += (int)(blockIdx.y * gridDim.x);
+    s(held, group);
 }
 
 template <typename T>
@@ -300,7 +302,10 @@ static BwdPlan plan_bwd(DzPass pass, int B, int d_in, long long cols, long long 
 template <typename T, class P, class Q>
 static srigl_status launch_gradients(const DensePlans& plans, const P& of_x, bool want_x, const Q& of_W, bool want_W, const SumChunks& sums, hipStream_t st) {
     if (want_x && want_W && plans.together && of_x.M > 0 && of_W.M > 0) return launch_dense_two<T>(of_x, of_W, sums, plans.dx.tile, st);
-    if (sums.groups() > 0) hipLaunchKernelGGL(k_sum_chunks, dim3((unsigned)sums.groups()), dim3(256), 0, st, sums);
+    if (sums.groups() > 0) {
+        const GridLayers grid = grid_layers(sums.groups(), 256);
+        hipLaunchKernelGGL(k_sum_chunks, dim3(grid.x, grid.times), dim3(256), 0, st, sums);
+    }
     if (hip_ok(hipGetLastError()) != SRIGL_OK) return SRIGL_ERR_HIP;
     const srigl_status rc = want_x ? launch_dense<T, false>(of_x, plans.dx.tile, st) : SRIGL_OK;
     return rc == SRIGL_OK && want_W ? launch_dense<T, false>(of_W, plans.dW.tile, st) : rc;

@@ -2,7 +2,7 @@
 import pytest
 import torch
 
-from paper_2305_02299_amd import StructuredLinear
+from paper_2305_02299_amd import GatedLinear, StructuredLinear
 from paper_2305_02299_amd import binding as B_
 
 pytestmark = pytest.mark.gpu
@@ -57,3 +57,46 @@ def test_a_result_in_the_memory_of_the_bias_or_the_list():
 def _over(t, n):
     """A float [1, n] that begins where t does"""
     return torch.empty(0, dtype=torch.float32, device="cuda").set_(t.view(torch.float32).untyped_storage(), 0, (1, n))
+
+
+# ---- more workgroups than one dimension of a grid holds (2^32 threads) ----
+def _same_everywhere(got, want, rows=1 << 25):
+    """got [n, ...] against want(first, behind), in pieces"""
+    return all(torch.equal(got[k:k + rows], want(k, min(k + rows, got.shape[0]))) for k in range(0, got.shape[0], rows))
+
+
+@pytest.mark.parametrize("gated", [False, True])
+def test_neurons_by_the_hundred_million(gated):
+    n, d_in = (1 << 28) + 37, 8
+    W = torch.empty(n, d_in, device="cuda", dtype=torch.bfloat16).random_(-2, 3)
+    x = torch.tensor([[1, 2, 0, -1, 3, 1, -2, 1], [0, 1, 1, 2, -1, 0, 1, 3]], device="cuda", dtype=torch.bfloat16)
+    want = lambda a, b: (W[a:b].float() @ x.float().T).bfloat16()  # noqa: E731  (whole numbers: exact)
+    if not gated:
+        y = StructuredLinear(d_in, n, W).forward(x)
+        for r in range(2):
+            assert _same_everywhere(y[r], lambda a, b: want(a, b)[:, r])
+        return
+    h, g, u = GatedLinear(d_in, n, W, W, act=B_.ACT_NONE).forward(x, save=True)
+    for r in range(2):
+        assert _same_everywhere(g[r], lambda a, b: want(a, b)[:, r]) and torch.equal(g[r], u[r])
+        assert _same_everywhere(h[r], lambda a, b: want(a, b)[:, r] * want(a, b)[:, r])
+
+
+@pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16])
+def test_rows_by_the_thousand_million(dtype):
+    """2^30 rows, the most that a call takes, of one neuron."""
+    B, d_in = 1 << 30, 8
+    x = torch.empty(B, d_in, device="cuda", dtype=dtype).random_(-2, 3)
+    W = torch.tensor([[1, -2, 0, 1, 3, 1, -2, 2]], device="cuda", dtype=dtype)
+    y = StructuredLinear(d_in, 1, W).forward(x)
+    assert _same_everywhere(y, lambda a, b: (x[a:b].float() @ W.float().T).to(dtype))
+
+
+def test_bias_sums_of_the_most_neurons():
+    n, d_in = 1 << 29, 1
+    dh, g, u = (torch.empty(1, n, device="cuda", dtype=torch.bfloat16).random_(-3, 4) for _ in range(3))
+    x, W = torch.ones(1, d_in, device="cuda", dtype=torch.bfloat16), torch.empty(1, 1, device="cuda", dtype=torch.bfloat16)
+    dbg, dbu = (torch.full((n,), 77.0, device="cuda") for _ in range(2))
+    ws = torch.empty(B_.srigl_gated_bwd_workspace_bytes(1, d_in, n, B_.BF16), dtype=torch.uint8, device="cuda")
+    B_.srigl_gated_linear_bwd(dh, x, 1, d_in, W, W, n, g, u, None, None, None, dbg, dbu, ws, B_.ACT_NONE)
+    assert torch.equal(dbg, (dh * u)[0].float()) and torch.equal(dbu, (dh * g)[0].float())
