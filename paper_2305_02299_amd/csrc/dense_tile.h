@@ -961,6 +961,46 @@ __global__ __launch_bounds__(WGM * WGN * 64) void k_dense_two(P p, Q q, int p_wg
     }
 }
 
+// ---- ablated columns where the stored neurons' are written one by one (few rows of x, and the join of parts) ----
+// first place in the ascending list whose entry is >= c, by a whole wavefront: a trip to memory for each 6 bits of the list's length
+__device__ __forceinline__ int wave_place_of(const int32_t* active, int n_active, int c) {
+    const int lane = threadIdx.x & 63;
+    int lo = 0, hi = n_active;   // the place is one of lo .. hi
+    while (lo < hi) {
+        const int step = (hi - lo + 63) >> 6, at = lo + (lane + 1) * step - 1;
+        lo += __popcll(__ballot(at < hi && active[min(at, hi - 1)] < c)) * step;
+        hi = min(hi, lo + step - 1);
+    }
+    return lo;
+}
+// They have workgroups of their own, NT columns and kAblatedRows rows each, in front of the others in the same launch: a thread its column, whatever run of neighbours it stands in.  (The thread of the neuron
+// behind a run wrote it, an element after the other, 0.13 to 0.3 us each, since the residual may be y: 4096 -> 16384 bf16 at one row, half of the neurons ablated at one end, 1140 us and at random 16.7, now 16.8 and 17.0;
+// in the kernel trace, at random, 3072 -> 768 with 538 stored at 16 rows 7.2 and now 6.7, 768 -> 768 with a fifth ablated at 64 11.6 and 7.1, the join of 2048 -> 1024 at 40 5.8 and 4.7; with short lines the search is what is
+// waited for: 128 -> 12000 at 8 rows 4.2 and 4.6.)
+constexpr int kAblatedRows = 16;
+template <int NT, class Out> inline long long ablated_groups(int B, const Out& out) {
+    if constexpr (Out::kListed)
+        if (out.active) return ((out.d_out + (long long)NT - 1) / NT) * ((B + kAblatedRows - 1ll) / kAblatedRows);
+    return 0;
+}
+template <int NT, class Out>
+__device__ __forceinline__ void write_ablated(int group, int B, const Out& out) {
+    __shared__ int stored[NT];
+    const int tid = threadIdx.x, slices = (int)((out.d_out + (long long)NT - 1) / NT), c0 = group % slices * NT, c = c0 + tid;
+    const int m0 = group / slices * kAblatedRows, m1 = min(m0 + kAblatedRows, B);
+    const bool there = c < out.d_out;
+    const float flat = out.ablated_value(there ? c : 0);
+    stored[tid] = 0;
+    const int from = wave_place_of(out.active, out.n_active, c0);
+    __syncthreads();
+    if (from + (long long)tid < out.n_active) {   // (no more than NT of them stand in NT columns)
+        const long long k = (long long)out.active[from + tid] - c0;
+        if (k >= 0 && k < NT) stored[k] = 1;
+    }
+    __syncthreads();
+    if (there && !stored[tid]) out.template ablated_rows<kAblatedRows>(c, m0, m1, flat);
+}
+
 // ---- joining the parts' sums: a thread takes V columns of a row; eight parts' values are requested together, so that it waits for memory once or twice ----
 template <int V, bool PAIR, class P>
 __device__ __forceinline__ void dense_join(long long item, P& p) {
@@ -990,8 +1030,16 @@ __device__ __forceinline__ void dense_join(long long item, P& p) {
     if constexpr (PAIR) p.out.template row<V>(m, c, valid, v, w);
     else p.out.template row<V>(m, c, valid, v);
 }
-template <int V, bool PAIR, class P>
-__global__ __launch_bounds__(256) void k_dense_join(P p) { dense_join<V, PAIR>((long long)blockIdx.x * 256 + threadIdx.x, p); }
+template <bool PAIR, class P>
+__global__ __launch_bounds__(256) void k_dense_join(P p) { dense_join<4, PAIR>((long long)blockIdx.x * 256 + threadIdx.x, p); }
+// with a list a neuron to a thread, behind the ablated columns' workgroups
+template <class P>
+__global__ __launch_bounds__(256) void k_dense_join_listed(P p, int ablated) {
+    int id = blockIdx.x;
+    if (blockIdx.y) id += (int)(blockIdx.y * gridDim.x);
+    if (id < ablated) write_ablated<256>(id, p.M, p.out);
+    else dense_join<1, false>((long long)(id - ablated) * 256 + threadIdx.x, p);
+}
 template <class P, class Q>
 __global__ __launch_bounds__(256) void k_dense_join_two(P p, Q q, unsigned p_groups) {
     if (blockIdx.x < p_groups) dense_join<4, false>((long long)blockIdx.x * 256 + threadIdx.x, p);
@@ -1018,12 +1066,15 @@ static srigl_status launch_tiles(const DenseProduct<OA, OB, Out>& p, hipStream_t
     const GridLayers grid = grid_layers(n_wg, WGM * WGN * 64);
     hipLaunchKernelGGL(kern, dim3(grid.x, (unsigned)p.parts, grid.times), dim3(WGM * WGN * 64), lds, st, p);
     if (p.parts > 1) {
-        bool one = false;   // a neuron to a thread, which writes the ablated columns in front of its own too
-        if constexpr (Out::kListed) {
-            one = p.out.active != nullptr;
-            if (one) hipLaunchKernelGGL((k_dense_join<1, PAIR, P>), dim3((unsigned)join_groups(p, 1)), dim3(256), 0, st, p);
-        }
-        if (!one) hipLaunchKernelGGL((k_dense_join<4, PAIR, P>), dim3((unsigned)join_groups(p, 4)), dim3(256), 0, st, p);
+        if constexpr (Out::kListed)
+            if (p.out.active) {
+                const long long ablated = ablated_groups<256>(p.M, p.out), all = ablated + join_groups(p, 1);
+                if (all > kMostGroups) return SRIGL_ERR_UNSUPPORTED;
+                const GridLayers layers = grid_layers(all, 256);
+                hipLaunchKernelGGL((k_dense_join_listed<P>), dim3(layers.x, layers.times), dim3(256), 0, st, p, (int)ablated);
+                return hip_ok(hipGetLastError());
+            }
+        hipLaunchKernelGGL((k_dense_join<PAIR, P>), dim3((unsigned)join_groups(p, 4)), dim3(256), 0, st, p);
     }
     return hip_ok(hipGetLastError());
 }
@@ -1105,15 +1156,16 @@ __device__ __forceinline__ void few_mma(f32x4_acc_t& acc, const uint4& a, const 
 
 // NB: blocks of 16 rows of x; UNITS of 128 bytes of a line requested together
 template <typename T, int NB, int NW, bool PAIR, int UNITS, class Out>
-__global__ __launch_bounds__(NW * 64) void k_dense_few(const T* __restrict__ x, int B, int K, const T* __restrict__ W, long long to_second, int n, int rows, Out out) {
+__global__ __launch_bounds__(NW * 64) void k_dense_few(const T* __restrict__ x, int B, int K, const T* __restrict__ W, long long to_second, int n, int rows, int ablated, Out out) {
     constexpr int MATS = PAIR ? 2 : 1, STEP = 64 / (int)sizeof(T), UNIT = 2 * STEP, P = kPiece<T>;
     __shared__ float sums[NW][MATS][16][17];   // [neuron][row of x], of 16 rows of x at a time
     const int lane = threadIdx.x & 63, wv = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-    int s0 = (int)blockIdx.x * rows;
-    if (blockIdx.y) {
-        s0 += (int)(blockIdx.y * gridDim.x) * rows;
-        if (s0 >= n) return;
-    }
+    int id = blockIdx.x;
+    if (blockIdx.y) id += (int)(blockIdx.y * gridDim.x);
+    if constexpr (Out::kListed)
+        if (id < ablated) return write_ablated<NW * 64>(id, B, out);
+    if (id - ablated > (n - 1) / rows) return;   // (layers of a grid may end behind the last one)
+    const int s0 = (id - ablated) * rows;
     const T *w[MATS], *xr[NB];
     const int off = (lane >> 4) * P;
     w[0] = W + (size_t)min(s0 + min(lane & 15, rows - 1), n - 1) * K + off;
@@ -1184,12 +1236,14 @@ static srigl_status launch_few(const T* x, int B, int K, const T* W, long long t
     // 16, 1024 -> 1024 2.7 and 3.0, but 768 -> 3072 3.9 and 3.2.
     const int rows = n >= 2048 ? 16 : 4;
     const bool wide = (long long)K * (int)sizeof(T) >= 20 * 128;   // eight wavefronts to a line, else four (bf16 4096 -> 16384 at one row 24.8 us, 27.3 with four)
-    const GridLayers layers = grid_layers((n + (long long)rows - 1) / rows, wide ? 512 : 256);
+    const long long ablated = wide ? ablated_groups<512>(B, out) : ablated_groups<256>(B, out), all = ablated + (n + (long long)rows - 1) / rows;
+    if (all > kMostGroups) return SRIGL_ERR_UNSUPPORTED;
+    const GridLayers layers = grid_layers(all, wide ? 512 : 256);
     const dim3 grid(layers.x, layers.times);
 #define SRIGL_FEW(NB, UNITS) \
     do { \
-        if (wide) hipLaunchKernelGGL((k_dense_few<T, NB, 8, PAIR, UNITS, Out>), grid, dim3(512), 0, st, x, B, K, W, to_second, n, rows, out); \
-        else hipLaunchKernelGGL((k_dense_few<T, NB, 4, PAIR, UNITS, Out>), grid, dim3(256), 0, st, x, B, K, W, to_second, n, rows, out); \
+        if (wide) hipLaunchKernelGGL((k_dense_few<T, NB, 8, PAIR, UNITS, Out>), grid, dim3(512), 0, st, x, B, K, W, to_second, n, rows, (int)ablated, out); \
+        else hipLaunchKernelGGL((k_dense_few<T, NB, 4, PAIR, UNITS, Out>), grid, dim3(256), 0, st, x, B, K, W, to_second, n, rows, (int)ablated, out); \
     } while (0)
     if (B <= 16) SRIGL_FEW(1, 4);
     else if (B <= 32) SRIGL_FEW(2, PAIR ? 2 : 3);

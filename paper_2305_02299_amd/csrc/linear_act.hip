@@ -222,13 +222,17 @@ struct LinearOut {
         }
         store_values<TY, V>(y + at, v, valid, first);
     }
-    // the ablated columns lo .. hi - 1
-    __device__ void ablated(int m, int lo, int hi) {
-        for (int c = max(lo, 0); c < min(hi, d_out); ++c) {
-            const size_t at = (size_t)m * d_out + c;
-            const float v = act_value(bias ? bias[c] : 0.0f, act);
-            y[at] = from_float<TY>(residual ? v + to_float(residual[at]) : v);
-        }
+    __device__ float ablated_value(int c) const { return act_value(bias ? bias[c] : 0.0f, act); }
+    // rows m0 .. m1 - 1, ROWS at most, of an ablated column; the residual's values are requested together
+    template <int ROWS> __device__ void ablated_rows(int c, int m0, int m1, float flat) const {
+        TY r[ROWS] = {};
+        if (residual)
+#pragma unroll
+            for (int k = 0; k < ROWS; ++k)
+                if (m0 + k < m1) r[k] = residual[(size_t)(m0 + k) * d_out + c];
+#pragma unroll
+        for (int k = 0; k < ROWS; ++k)
+            if (m0 + k < m1) y[(size_t)(m0 + k) * d_out + c] = from_float<TY>(residual ? flat + to_float(r[k]) : flat);
     }
     template <int V> __device__ void row(int m, int s, int valid, float (&v)[V]) {
 #pragma unroll
@@ -246,17 +250,14 @@ struct LinearOut {
             store_values<TY, V>(y + at, v, valid);
             return;
         }
-        // stored neuron s + q writes the ablated columns in front of it too, the last one those behind it
 #pragma unroll
         for (int q = 0; q < V; ++q) {
             if (q >= valid) break;
             const int c = active[s + q];
-            ablated(m, s + q > 0 ? active[s + q - 1] + 1 : 0, c);
             if ((unsigned)c < (unsigned)d_out) {
                 const size_t at = (size_t)m * d_out + c;
                 y[at] = from_float<TY>(residual ? v[q] + to_float(residual[at]) : v[q]);
             }
-            if (s + q == n_active - 1) ablated(m, c + 1, d_out);
         }
     }
 };

@@ -100,3 +100,45 @@ def test_bias_sums_of_the_most_neurons():
     ws = torch.empty(B_.srigl_gated_bwd_workspace_bytes(1, d_in, n, B_.BF16), dtype=torch.uint8, device="cuda")
     B_.srigl_gated_linear_bwd(dh, x, 1, d_in, W, W, n, g, u, None, None, None, dbg, dbu, ws, B_.ACT_NONE)
     assert torch.equal(dbg, (dh * u)[0].float()) and torch.equal(dbu, (dh * g)[0].float())
+
+
+# ---- neighbours ablated together ----
+@pytest.mark.parametrize("out", [torch.float32, torch.bfloat16])
+@pytest.mark.parametrize("B,d_in", [(1, 72), (16, 200), (17, 72), (64, 136), (40, 2056), (300, 4096)])
+@pytest.mark.parametrize("kind", ["first", "last", "one in the middle", "both ends", "blocks", "every 300th", "all but one"])
+def test_runs_of_ablated_neurons(kind, B, d_in, out):
+    """Every column of every row, from runs of any length, with a residual in place and without: whole numbers, exact."""
+    d_out = 9001
+    gen = torch.Generator().manual_seed(B)
+    stored = {"first": torch.arange(33), "last": torch.arange(d_out - 5, d_out), "one in the middle": torch.tensor([4500]), "both ends": torch.tensor([0, d_out - 1]),
+              "blocks": torch.cat([torch.arange(256, 512), torch.arange(1024, 1040), torch.arange(8960, 8992)]), "every 300th": torch.arange(7, d_out, 300),
+              "all but one": torch.cat([torch.arange(2000), torch.arange(2001, d_out)])}[kind]
+    W, x, bias, residual = (torch.randint(-2, 3, s, generator=gen).float() for s in ((len(stored), d_in), (B, d_in), (d_out,), (B, d_out)))
+    t = torch.bfloat16
+    layer = StructuredLinear(d_in, d_out, W.to(t).cuda(), stored.int().cuda(), bias.cuda())
+    want = bias.expand(B, d_out).clone()
+    want[:, stored] += x @ W.T
+    want = want.clamp(min=0)
+    assert torch.equal(layer.forward(x.to(t).cuda(), act=B_.ACT_RELU, out_dtype=out).cpu(), want.to(out))
+    y = residual.to(out).cuda()
+    got, z = layer.forward(x.to(t).cuda(), act=B_.ACT_RELU, residual=y, y=y, save=True)
+    assert torch.equal(y.cpu(), (want + residual).to(out)) and torch.equal(z.cpu(), (x @ W.T + bias[stored]).to(t))
+
+
+@pytest.mark.parametrize("B,d_in", [(1, 64), (16, 64), (40, 4096)])
+def test_a_run_of_millions_is_shared_out(B, d_in):
+    """One neuron of 4 million: a tenth of a second is two hundred times what the columns take and a fifth of what one thread took for a row's."""
+    d_out = (1 << 22) + 5
+    bias = torch.empty(d_out, device="cuda").random_(-3, 4)
+    layer = StructuredLinear(d_in, d_out, torch.ones(1, d_in, device="cuda", dtype=torch.bfloat16), torch.tensor([d_out // 3], device="cuda", dtype=torch.int32), bias)
+    x = torch.ones(B, d_in, device="cuda", dtype=torch.bfloat16)
+    y = layer.forward(x, act=B_.ACT_RELU)
+    want = bias.clone()
+    want[d_out // 3] += d_in
+    assert torch.equal(y, want.clamp(min=0).bfloat16().expand(B, d_out))
+    start, end = torch.cuda.Event(enable_timing=True), torch.cuda.Event(enable_timing=True)
+    start.record()
+    layer.forward(x, act=B_.ACT_RELU)
+    end.record()
+    torch.cuda.synchronize()
+    assert start.elapsed_time(end) < 100
