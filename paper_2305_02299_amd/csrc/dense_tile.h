@@ -962,10 +962,9 @@ __global__ __launch_bounds__(WGM * WGN * 64) void k_dense_two(P p, Q q, int p_wg
 }
 
 // ---- ablated columns where the stored neurons' are written one by one (few rows of x, and the join of parts) ----
-// first place in the ascending list whose entry is >= c, by a whole wavefront: a trip to memory for each 6 bits of the list's length
-__device__ __forceinline__ int wave_place_of(const int32_t* active, int n_active, int c) {
+// the place lo .. hi in the ascending list in front of which all entries are < c, by a whole wavefront: a trip to memory for each 6 bits of hi - lo
+__device__ __forceinline__ int wave_place_of(const int32_t* active, int lo, int hi, int c) {
     const int lane = threadIdx.x & 63;
-    int lo = 0, hi = n_active;   // the place is one of lo .. hi
     while (lo < hi) {
         const int step = (hi - lo + 63) >> 6, at = lo + (lane + 1) * step - 1;
         lo += __popcll(__ballot(at < hi && active[min(at, hi - 1)] < c)) * step;
@@ -991,12 +990,21 @@ __device__ __forceinline__ void write_ablated(int group, int B, const Out& out) 
     const bool there = c < out.d_out;
     const float flat = out.ablated_value(there ? c : 0);
     stored[tid] = 0;
-    const int from = wave_place_of(out.active, out.n_active, c0);
-    __syncthreads();
-    if (from + (long long)tid < out.n_active) {   // (no more than NT of them stand in NT columns)
-        const long long k = (long long)out.active[from + tid] - c0;
-        if (k >= 0 && k < NT) stored[k] = 1;
+    // The slice's neurons begin at their column's number in the list less the ablated columns in front, some of all that there are: where these are few, everything from the first possible place on is read
+    // (one trip; 1001 -> 777 with a tenth ablated at 37 rows, the join of parts 5.0 us with a search, 4.4 without).
+    const int n = out.n_active, gone = out.d_out - n;
+    int lo = max(c0 - gone, 0), hi = min(c0, n);
+    if (hi - lo > 3 * NT) hi = lo = wave_place_of(out.active, lo, hi, c0);
+    int entry[4];
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+        const int k = lo + i * NT + tid;
+        entry[i] = k < min(hi + NT, n) ? out.active[k] : -1;
     }
+    __syncthreads();
+#pragma unroll
+    for (int i = 0; i < 4; ++i)
+        if (entry[i] >= c0 && entry[i] - c0 < NT) stored[entry[i] - c0] = 1;
     __syncthreads();
     if (there && !stored[tid]) out.template ablated_rows<kAblatedRows>(c, m0, m1, flat);
 }
