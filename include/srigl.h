@@ -483,7 +483,7 @@ srigl_status srigl_structured_linear_fwd_split(const void* x, srigl_dtype x_dtyp
  *
  * srigl_structured_linear_fwd_act:
  *   z[b][s] = bias[active[s]] + sum_j Wd[s][j] x[b][j];  y[b][active[s]] = act(z[b][s]) + residual[b][active[s]];  other columns: act(bias[c]) + residual[b][c].
- *   active, bias as in srigl_structured_linear_fwd; residual[B][d_out] of y_dtype or NULL, may be y itself; y[B][d_out] of y_dtype, the storage type or fp32; z
+ *   active (strictly ascending), bias as in srigl_structured_linear_fwd; residual[B][d_out] of y_dtype or NULL, may be y itself; y[B][d_out] of y_dtype, the storage type or fp32; z
  *   (may be NULL): [B][n_active] of the storage type, what the backward pass takes.
  * srigl_structured_linear_bwd: with dz[b][s] = dy[b][active[s]] act'(z[b][s]),
  *   dx[B][d_in] = dz Wd and dWd[n_active][d_in] = dz^T x of the storage type, dbias[d_out] fp32: sum_b dz[b][s] at active[s], act'(bias[c]) sum_b dy[b][c] at the

@@ -11,7 +11,7 @@ namespace srigl {
 // Expected time (us) of a product in a tile and `parts` parts of K: a fixed part, a part a round of workgroups over the compute units and, by 1000 elements of K, a part a round and one that follows how
 // full the rounds are, a part per million results, a second launch and the parts' sums (a million of them written and read) where there are several.  Non-negative least squares on the relative error of
 // 145000 timings in graphs, every tile and 1 to 16 parts of 26000 random products (17 to 2048 rows, 100 to 4096 wide, 100 to 16384 neurons): 4 to 10 % a timing; the tile and parts of smallest time are 0.3
-// to 2 % behind the fastest on average by kind and type, 9 % at worst in 95 of 100, 34 % at worst.
+// to 2 % behind the fastest on average by kind and type, 9 % at worst in 95 of 100, 34 % at worst.  (fp32 was timed with the parts of values cut off in place of rounded, 0 to 7 % faster.)
 struct DenseModel {
     int kind, f32, direct, tile, slots;
     float us[7];   // fixed, round, per_k, per_k_full, results, second, part

@@ -169,7 +169,7 @@ def fold_mlp(layer1: CondensedLinear, layer2: CondensedLinear, act: int) -> Cond
 @dataclass
 class StructuredLinear:
     """One layer in the structured-only form on the GPU: Wd [n_active, d_in] (fp32 or bf16 storage) are the rows of the neurons that are not ablated,
-    active [n_active] int32 their columns of the result (None: every neuron is stored), bias [d_out] fp32 or None.  Forward with activation and residual, and
+    active [n_active] int32 their columns of the result, strictly ascending (None: every neuron is stored), bias [d_out] fp32 or None.  Forward with activation and residual, and
     the gradients; dWd of a layer without ablated neurons in fp32 is the gradient that srigl_mask_update ranks.  Results and scratch come from torch's
     allocator, in the order of the current stream; no autograd graph is kept."""
 
